@@ -315,6 +315,102 @@ int32_t lstmss_sgd_update(const lstmss_dims *d, void *W, float *b, const float *
 int32_t lstmss_mse_grad(const lstmss_dims *d, const void *h, const float *y, float *dH,
                         double *loss, void *stream);
 
+/* Language-model operators around the layers: what turns tokens into the
+ * stack's input and the stack's output into a loss.  All are batch-last.  A
+ * token or target outside [0, V) is padding: it takes no part (its column of x
+ * is zero, it adds to no gradient, its logp, loss and dlogits are zero,
+ * whatever its logits hold).
+ * Sizes: T steps, batch B, I features of the embedding, vocabulary V; dtype is
+ * the storage type of the embedding table and x, or of the logits.  T * B and
+ * V below 2^31 - 65536, V * max(B, I) below 2^31, T * B * max(V, I) below 2^40.
+ * The loss calls do not use I, which must be positive all the same. */
+typedef struct {
+    int32_t T, B, I, V;
+    int32_t dtype;
+} lstmss_tokens;
+
+/* Dropout whose mask is a function of the element's index and is never
+ * stored: element e takes the 16 bits number (g mod 8) of the 128 that
+ * Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy
+ * as 1, 2, 3", 2011) gives for counter floor(g / 8) (low and high half in
+ * counter words 0 and 1, words 2 and 3 zero) and key `seed` (low half in key
+ * word 0), g = offset + (period > 0 ? e mod period : e); bits 16k .. 16k+15
+ * come from output word k / 2, low half first.  With thr = p * 65536 rounded
+ * to nearest (ties to even, at most 65535) the element is dropped (+0, whatever it holds)
+ * where its bits are below thr and otherwise multiplied by 65536 / (65536 -
+ * thr), formed in fp32: the mean is kept for the rounded p, not the given one.
+ *   p       in [0, 1)
+ *   offset  a multiple of 8: what earlier calls with this seed have taken,
+ *           each rounded up to a multiple of 8
+ *   period  0, or the length after which the mask repeats, >= 1: H * B on
+ *           [T][H][B] is one mask for all steps */
+typedef struct {
+    float p;
+    uint64_t seed, offset;
+    int64_t period;
+} lstmss_drop;
+
+/* y = dropout(x) over n elements of `dtype`; y may be x.  The gradient of x
+ * is the same call on the gradient of y (whose type may be another: the mask
+ * depends on the index alone). */
+int32_t lstmss_dropout(int64_t n, int32_t dtype, const lstmss_drop *drop, const void *x, void *y,
+                       void *stream);
+
+/* Embedding lookup: x[t][i][b] = scale * E[tokens[t][b]][i], then dropout over
+ * x when drop is not NULL; formed in fp32, rounded once.
+ *   E [V][I] dtype, tokens [T][B] int32, x [T][I][B] dtype (must not overlap E). */
+int32_t lstmss_embed(const lstmss_tokens *d, const void *E, const int32_t *tokens, float scale,
+                     const lstmss_drop *drop, void *x, void *stream);
+
+/* Its gradient: dE[v][i] = scale * the sum of dropout(dX)[t][i][b] over the
+ * (t, b) with token v, in fp32, in an order that the tokens alone decide (the
+ * tokens are sorted, equal ones by position: no atomics).
+ *   dX [T][I][B] fp32, dE [V][I] fp32; drop as given to lstmss_embed, or NULL
+ *   accumulate  0: dE is overwritten (rows of absent tokens with zero);
+ *               1: the sums are added to it (rows of absent tokens are not
+ *               touched), as for a table that is also the output layer's, or,
+ *               with E as dE and scale times minus the learning rate, SGD
+ *   ws  lstmss_embed_grad_workspace_bytes(d) bytes.  d->dtype is not used. */
+int64_t lstmss_embed_grad_workspace_bytes(const lstmss_tokens *d);
+int32_t lstmss_embed_grad(const lstmss_tokens *d, const int32_t *tokens, const float *dX,
+                          float scale, const lstmss_drop *drop, int32_t accumulate, float *dE,
+                          void *ws, size_t ws_bytes, void *stream);
+
+/* Losses on logits [T][V][B] (dtype) against targets [T][B] int32; with
+ * logp[t][b] = log softmax(logits[t][:][b])[targets[t][b]] and weights w[t][b]
+ * (fp32, NULL = 1; a token of weight 0 is padding too):
+ *   lstmss_token_logp   logp alone (scoring, and the old and the reference
+ *                       model's logp of the policy loss)
+ *   lstmss_xent         L = -scale * sum of w * logp
+ *   lstmss_policy_loss  L = scale * sum of w * l,  l = -min(r * adv,
+ *                       clip(r, 1 - clip_low, 1 + clip_high) * adv)
+ *                       + kl * (exp(q) - q - 1),  r = exp(logp - logp_old),
+ *                       q = logp_ref - logp.  logp_old NULL: logp itself, taken
+ *                       as a constant (r = 1 with gradient adv).  logp_ref NULL:
+ *                       no KL term (kl must be 0).
+ * Outputs: loss fp32 [1] (summed in fp64 in a fixed order) or NULL, logp
+ * [T][B] fp32 or NULL (lstmss_token_logp: required), dlogits [T][V][B] dtype
+ * or NULL = dL/dlogits; dlogits may be logits itself.  Where r * adv equals the
+ * clipped product the gradient is the unclipped one's.
+ * The softmax's maximum is exact and its sum of fp32; per-token terms are fp64.
+ *   ws  lstmss_loss_workspace_bytes(d) bytes. */
+typedef struct {
+    float clip_low, clip_high; /* >= 0, clip_low <= 1 */
+    float kl;                  /* >= 0 */
+    float scale;
+} lstmss_policy;
+
+int64_t lstmss_loss_workspace_bytes(const lstmss_tokens *d);
+int32_t lstmss_token_logp(const lstmss_tokens *d, const void *logits, const int32_t *targets,
+                          float *logp, void *ws, size_t ws_bytes, void *stream);
+int32_t lstmss_xent(const lstmss_tokens *d, const void *logits, const int32_t *targets,
+                    const float *weights, float scale, float *loss, float *logp, void *dlogits,
+                    void *ws, size_t ws_bytes, void *stream);
+int32_t lstmss_policy_loss(const lstmss_tokens *d, const lstmss_policy *p, const void *logits,
+                           const int32_t *targets, const float *logp_old, const float *logp_ref,
+                           const float *adv, const float *weights, float *loss, float *logp,
+                           void *dlogits, void *ws, size_t ws_bytes, void *stream);
+
 /* Execution options (results are identical under every setting):
  *   LSTMSS_OPT_GRAPHS  0 or 1 (default), without effect: every call is
  *                      enqueued directly, never recorded into a HIP graph
@@ -395,7 +491,8 @@ enum {
     LSTMSS_KERNEL_GATES = 0,       /* gate gradient + score/select/compact (or dense) */
     LSTMSS_KERNEL_DATA_GRAD = 1,   /* [dx; dh] = W_c^T dG_c, split-K partials */
     LSTMSS_KERNEL_WEIGHT_GRAD = 2, /* dW[kept rows] += dG_c [x; h]^T */
-    LSTMSS_KERNEL_AUX = 3,         /* zero fills, final reductions and copies */
+    LSTMSS_KERNEL_AUX = 3,         /* zero fills, final reductions and copies; the
+                                      language-model operators */
     LSTMSS_KERNEL_FORWARD = 4,     /* forward step */
     LSTMSS_KERNEL_KINDS = 5
 };

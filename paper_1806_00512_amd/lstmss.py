@@ -9,6 +9,8 @@ current stream.  The entry points mirror include/lstmss.h:
   bwd_structsparse       -> lstm_bwd_structsparse
   select_compact         -> lstmss_select_compact
   cache_bytes / kept_rows / index_entries / workspace_bytes -> the size queries
+  embed, embed_grad, dropout         -> lstmss_embed, lstmss_embed_grad, lstmss_dropout
+  token_logp, xent, policy_loss      -> lstmss_token_logp, lstmss_xent, lstmss_policy_loss
 
 Loading fails loudly (RuntimeError) when liblstmss.so has not been built;
 there is no fallback implementation.
@@ -36,7 +38,9 @@ SYMBOLS = ("lstmss_version", "lstmss_strerror", "lstmss_last_error", "lstmss_cac
            "lstmss_bidir_join", "lstmss_bidir_workspace_bytes", "lstm_bwd_bidir",
            "lstm_fwd_cache", "lstm_bwd_dense",
            "lstm_bwd_structsparse", "lstmss_select_workspace_bytes", "lstmss_select_compact",
-           "lstmss_select_compact_noalloc", "lstmss_set_option",
+           "lstmss_select_compact_noalloc", "lstmss_dropout", "lstmss_embed",
+           "lstmss_embed_grad_workspace_bytes", "lstmss_embed_grad", "lstmss_loss_workspace_bytes",
+           "lstmss_token_logp", "lstmss_xent", "lstmss_policy_loss", "lstmss_set_option",
            "lstmss_timing_enable", "lstmss_timing_read", "lstmss_timing_reset")
 KERNEL_KINDS = {"gates_select_compact": 0, "data_grad_gemm": 1, "weight_grad_gemm": 2, "aux": 3,
                 "forward_step": 4}
@@ -50,6 +54,21 @@ class Dims(ctypes.Structure):
 class Structure(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("P", ctypes.c_int32), ("R", ctypes.c_int32),
                 ("My", ctypes.c_int32), ("Mx", ctypes.c_int32)]
+
+
+class Tokens(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("B", ctypes.c_int32), ("I", ctypes.c_int32),
+                ("V", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class Drop(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64),
+                ("period", ctypes.c_int64)]
+
+
+class Policy(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float),
+                ("kl", ctypes.c_float), ("scale", ctypes.c_float)]
 
 
 class LstmssError(RuntimeError):
@@ -118,6 +137,24 @@ def load():
     lib.lstmss_select_compact.restype = i32
     lib.lstmss_select_compact_noalloc.argtypes = [pd, f, ps, vp, vp, vp, vp, vp]
     lib.lstmss_select_compact_noalloc.restype = i32
+    pt, pr = ctypes.POINTER(Tokens), ctypes.POINTER(Drop)
+    lib.lstmss_dropout.argtypes = [i64, i32, pr, vp, vp, vp]
+    lib.lstmss_dropout.restype = i32
+    lib.lstmss_embed.argtypes = [pt, vp, vp, f, pr, vp, vp]
+    lib.lstmss_embed.restype = i32
+    lib.lstmss_embed_grad_workspace_bytes.argtypes = [pt]
+    lib.lstmss_embed_grad_workspace_bytes.restype = i64
+    lib.lstmss_embed_grad.argtypes = [pt, vp, vp, f, pr, i32, vp, vp, ctypes.c_size_t, vp]
+    lib.lstmss_embed_grad.restype = i32
+    lib.lstmss_loss_workspace_bytes.argtypes = [pt]
+    lib.lstmss_loss_workspace_bytes.restype = i64
+    lib.lstmss_token_logp.argtypes = [pt, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.lstmss_token_logp.restype = i32
+    lib.lstmss_xent.argtypes = [pt, vp, vp, vp, f, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.lstmss_xent.restype = i32
+    lib.lstmss_policy_loss.argtypes = [pt, ctypes.POINTER(Policy), vp, vp, vp, vp, vp, vp, vp, vp,
+                                       vp, vp, ctypes.c_size_t, vp]
+    lib.lstmss_policy_loss.restype = i32
     lib.lstmss_set_option.argtypes = [i32, i32]
     lib.lstmss_set_option.restype = i32
     lib.lstmss_timing_enable.argtypes = [i32]
@@ -539,6 +576,210 @@ def select_compact_noalloc(dG, dG_c, idx, scores=None, sparsity=0.5, P=4, R=8, s
         _ptr(dG_c, dG.dtype, name="dG_c"), _ptr(idx, torch.int32, name="idx"),
         _ptr(scores, torch.float64, name="scores"), _stream(stream))
     _check(rc, "lstmss_select_compact_noalloc")
+
+
+def drop(p, seed, offset=0, period=0) -> Drop:
+    """Dropout of the operators below: probability p, a 64-bit seed, the
+    elements that earlier calls with this seed took (a multiple of 8), and the
+    length after which the mask repeats (0: never)."""
+    if not 0 <= int(offset) < 2**64 or not -2**63 <= int(period) < 2**63:
+        raise ValueError("offset %d and period %d must fit 64 bits" % (offset, period))
+    return Drop(float(p), int(seed) & (2**64 - 1), int(offset), int(period))
+
+
+def _drop_ptr(d):
+    if d is None:
+        return None
+    if not isinstance(d, Drop):
+        raise TypeError("drop must be made by drop()")
+    return ctypes.byref(d)
+
+
+def _on(first, name, stream):
+    """The stream of a call whose tensors live where `first` does, as (torch stream, pointer)."""
+    if not isinstance(first, torch.Tensor):
+        raise TypeError("%s must be a torch tensor" % name)
+    if first.device.type != "cuda":
+        raise ValueError("%s must live on the GPU" % name)
+    if first.device.index != torch.cuda.current_device():
+        raise ValueError("%s lives on %s, which is not the current GPU" % (name, first.device))
+    s = stream if stream is not None else torch.cuda.current_stream()
+    if s.device != first.device:
+        raise ValueError("the stream is of %s, %s lives on %s" % (s.device, name, first.device))
+    return s, ctypes.c_void_p(s.cuda_stream)
+
+
+def _sizes(T, B, I, V, dtype) -> Tokens:
+    n = [int(k) for k in (T, B, I, V)]
+    if max(n) >= 2**31 or min(n) < -2**31:
+        raise ValueError("sizes %s must fit 32 bits" % n)
+    return Tokens(*n, _dt(dtype))
+
+
+def _near(dev, **tensors):
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.device != dev:
+            raise ValueError("%s lives on %s, expected %s" % (name, t.device, dev))
+
+
+def _new(shape, dtype, dev, s, stream):
+    """A tensor that work on stream s will use (s may not be the one it is allocated for)."""
+    t = torch.empty(shape, dtype=dtype, device=dev)
+    if stream is not None:
+        t.record_stream(s)
+    return t
+
+
+def _bytes(n, what):
+    _check(0 if n >= 0 else int(n), what)
+    return int(n)
+
+
+def dropout(x, drop, out=None, stream=None):
+    """x with dropout (see drop()), any shape; out may be x.  The gradient of x
+    is dropout(gradient of out, the same drop)."""
+    s, sp = _on(x, "x", stream)
+    dt = _dt(x.dtype)
+    if drop is None:
+        raise TypeError("drop must be made by drop()")
+    if out is None:
+        out = _new(x.shape, x.dtype, x.device, s, stream)
+    _near(x.device, out=out)
+    rc = load().lstmss_dropout(x.numel(), dt, _drop_ptr(drop), _ptr(x, name="x"),
+                               _ptr(out, x.dtype, x.shape, "out"), sp)
+    _check(rc, "lstmss_dropout")
+    return out
+
+
+def embed(tokens, E, scale=1.0, drop=None, out=None, stream=None):
+    """x [T][I][B] = scale * E[tokens] of tokens [T][B] (int32; outside [0, V): zeros)
+    and a table E [V][I] (fp32 or bf16), with dropout over x where drop is given."""
+    s, sp = _on(tokens, "tokens", stream)
+    _near(tokens.device, E=E, out=out)
+    if tokens.dim() != 2 or E.dim() != 2:
+        raise ValueError("tokens must be [T][B] and E [V][I]")
+    (T, B), (V, I) = tokens.shape, E.shape
+    d = _sizes(T, B, I, V, E.dtype)
+    if out is None:
+        out = _new((T, I, B), E.dtype, E.device, s, stream)
+    rc = load().lstmss_embed(ctypes.byref(d), _ptr(E, name="E"),
+                             _ptr(tokens, torch.int32, name="tokens"), float(scale),
+                             _drop_ptr(drop), _ptr(out, E.dtype, (T, I, B), "out"), sp)
+    _check(rc, "lstmss_embed")
+    return out
+
+
+def embed_grad_workspace_bytes(T, B, I, V) -> int:
+    d = _sizes(T, B, I, V, F32)
+    return _bytes(load().lstmss_embed_grad_workspace_bytes(ctypes.byref(d)),
+                  "lstmss_embed_grad_workspace_bytes")
+
+
+def embed_grad(tokens, dX, V, scale=1.0, drop=None, accumulate=False, dE=None, ws=None,
+               stream=None):
+    """Gradient of embed: dE [V][I] fp32 from dX [T][I][B] fp32, overwritten or
+    (accumulate, with dE given) added to."""
+    s, sp = _on(tokens, "tokens", stream)
+    _near(tokens.device, dX=dX, dE=dE, ws=ws)
+    if tokens.dim() != 2 or dX.dim() != 3:
+        raise ValueError("tokens must be [T][B] and dX [T][I][B]")
+    (T, B), I, V = tokens.shape, dX.shape[1], int(V)
+    d = _sizes(T, B, I, V, F32)
+    if dE is None:
+        if accumulate:
+            raise ValueError("accumulate needs dE")
+        dE = _new((V, I), torch.float32, dX.device, s, stream)
+    if ws is None:
+        ws = _new(embed_grad_workspace_bytes(T, B, I, V), torch.uint8, dX.device, s, stream)
+    rc = load().lstmss_embed_grad(ctypes.byref(d), _ptr(tokens, torch.int32, name="tokens"),
+                                  _ptr(dX, torch.float32, (T, I, B), "dX"), float(scale),
+                                  _drop_ptr(drop), 1 if accumulate else 0,
+                                  _ptr(dE, torch.float32, (V, I), "dE"),
+                                  _ptr(ws, torch.uint8, name="ws"), ws.numel(), sp)
+    _check(rc, "lstmss_embed_grad")
+    return dE
+
+
+def loss_workspace_bytes(T, B, V, dtype=F32) -> int:
+    """Workspace of token_logp, xent and policy_loss on logits [T][V][B]."""
+    d = _sizes(T, B, 1, V, dtype)
+    return _bytes(load().lstmss_loss_workspace_bytes(ctypes.byref(d)),
+                  "lstmss_loss_workspace_bytes")
+
+
+def _loss_args(logits, targets, ws, stream, **tokens):
+    """What the three loss calls share: sizes, workspace, stream, pointers."""
+    s, sp = _on(logits, "logits", stream)
+    _near(logits.device, targets=targets, ws=ws, **tokens)
+    if logits.dim() != 3:
+        raise ValueError("logits must be [T][V][B]")
+    T, V, B = logits.shape
+    d = _sizes(T, B, 1, V, logits.dtype)
+    if ws is None:
+        ws = _new(loss_workspace_bytes(T, B, V, logits.dtype), torch.uint8, logits.device, s,
+                  stream)
+    f32 = torch.float32
+    return (d, s, sp, ws, _ptr(logits, name="logits"),
+            _ptr(targets, torch.int32, (T, B), "targets"),
+            {k: _ptr(t, f32, (T, B), k) for k, t in tokens.items()})
+
+
+def _loss_out(logits, out, want_grad, s, stream):
+    T, V, B = logits.shape
+    o, dev = dict(out or {}), logits.device
+    for k, shape, dt in (("loss", (1,), torch.float32), ("logp", (T, B), torch.float32),
+                         ("dlogits", (T, V, B), logits.dtype)):
+        if o.get(k) is None and (want_grad or k != "dlogits"):
+            o[k] = _new(shape, dt, dev, s, stream)
+    _near(dev, **o)
+    return o, (_ptr(o["loss"], torch.float32, (1,), "loss"),
+               _ptr(o["logp"], torch.float32, (T, B), "logp"),
+               _ptr(o["dlogits"], logits.dtype, (T, V, B), "dlogits") if want_grad else None)
+
+
+def token_logp(logits, targets, logp=None, ws=None, stream=None):
+    """logp [T][B] fp32: log softmax over the middle axis of logits [T][V][B] (fp32
+    or bf16) at targets [T][B] (int32; outside [0, V): 0)."""
+    d, s, sp, ws, px, py, _ = _loss_args(logits, targets, ws, stream)
+    if logp is None:
+        logp = _new((d.T, d.B), torch.float32, logits.device, s, stream)
+    _near(logits.device, logp=logp)
+    rc = load().lstmss_token_logp(ctypes.byref(d), px, py,
+                                  _ptr(logp, torch.float32, (d.T, d.B), "logp"),
+                                  _ptr(ws, torch.uint8, name="ws"), ws.numel(), sp)
+    _check(rc, "lstmss_token_logp")
+    return logp
+
+
+def xent(logits, targets, weights=None, scale=None, want_grad=True, out=None, ws=None,
+         stream=None):
+    """Cross entropy -scale * sum of weights * logp (scale: 1 / B unless given).
+    Returns dict(loss [1], logp [T][B], dlogits like logits); out: tensors to
+    write those to (dlogits may be logits itself)."""
+    d, s, sp, ws, px, py, p = _loss_args(logits, targets, ws, stream, weights=weights)
+    o, (pl, pp, pg) = _loss_out(logits, out, want_grad, s, stream)
+    rc = load().lstmss_xent(ctypes.byref(d), px, py, p["weights"],
+                            1.0 / d.B if scale is None else float(scale), pl, pp, pg,
+                            _ptr(ws, torch.uint8, name="ws"), ws.numel(), sp)
+    _check(rc, "lstmss_xent")
+    return o
+
+
+def policy_loss(logits, targets, old, ref, adv, weights=None, clip_low=0.2, clip_high=0.2,
+                kl=0.0, scale=None, want_grad=True, out=None, ws=None, stream=None):
+    """Clipped policy loss with a KL term (see lstmss_policy_loss): old, ref (None:
+    the logits' own logp; no KL term), adv and weights are [T][B] fp32.  Returns
+    and takes the outputs of xent."""
+    d, s, sp, ws, px, py, p = _loss_args(logits, targets, ws, stream, old=old, ref=ref, adv=adv,
+                                         weights=weights)
+    o, (pl, pp, pg) = _loss_out(logits, out, want_grad, s, stream)
+    q = Policy(float(clip_low), float(clip_high), float(kl),
+               1.0 / d.B if scale is None else float(scale))
+    rc = load().lstmss_policy_loss(ctypes.byref(d), ctypes.byref(q), px, py, p["old"], p["ref"],
+                                   p["adv"], p["weights"], pl, pp, pg,
+                                   _ptr(ws, torch.uint8, name="ws"), ws.numel(), sp)
+    _check(rc, "lstmss_policy_loss")
+    return o
 
 
 def cache_views(cache, T, B, H, dtype):
