@@ -321,8 +321,9 @@ int32_t lstmss_mse_grad(const lstmss_dims *d, const void *h, const float *y, flo
  * is zero, it adds to no gradient, its logp, loss and dlogits are zero,
  * whatever its logits hold).
  * Sizes: T steps, batch B, I features of the embedding, vocabulary V; dtype is
- * the storage type of the embedding table and x, or of the logits.  T * B and
- * V below 2^31 - 65536, V * max(B, I) below 2^31, T * B * max(V, I) below 2^40.
+ * the storage type of the embedding table and x, or of the logits.  T at most
+ * 2^22, T * B below 2^29, V below 2^31 - 65536, V * B, V * I and I * B below
+ * 2^31, T * B * max(V, I) below 2^40.
  * The loss calls do not use I, which must be positive all the same. */
 typedef struct {
     int32_t T, B, I, V;
@@ -392,7 +393,7 @@ int32_t lstmss_embed_grad(const lstmss_tokens *d, const int32_t *tokens, const f
  * [T][B] fp32 or NULL (lstmss_token_logp: required), dlogits [T][V][B] dtype
  * or NULL = dL/dlogits; dlogits may be logits itself.  Where r * adv equals the
  * clipped product the gradient is the unclipped one's.
- * The softmax's maximum is exact and its sum of fp32; per-token terms are fp64.
+ * The softmax's sum is of fp32, per-token terms are of fp64.
  *   ws  lstmss_loss_workspace_bytes(d) bytes. */
 typedef struct {
     float clip_low, clip_high; /* >= 0, clip_low <= 1 */

@@ -2,100 +2,291 @@
 // the targets, per-token terms, gradient in the logits.
 //
 //   m = max_v x_v,  s = sum_v exp(x_v - m),  logp = x_y - m - log s
-//   dL/dx_v = dlogp * ([v = y] - exp(x_v - m) / s)
+//   dL/dx_v = dlogp * ([v = y] - exp(x_v - lse)),  lse = m + log s
+//
+// Three kernels: partial (m, s) of every column over a chunk of rows; the
+// per-token terms (the chunks' joined (m, s), logp, the loss, dlogp); the
+// gradient.  A step's logits are V * B elements in one piece, columns
+// fastest, so a thread that walks a piece in strides of whole rows keeps its
+// columns: their running (m, s), or their (lse, dlogp), stay in registers,
+// whatever B is.
 #include <algorithm>
+#include <cfloat>
+#include <numeric>
 
 #include "common.h"
 #include "language.h"
+#include "vec.h"
 
 namespace lstmss {
 
 namespace {
 
-// Running maximum and sum of exponentials of a column.
+constexpr int NT = 256; // threads of a work-group at most
+
+// Reference and sum of exponentials of a column: sum exp(x - m), where m is a
+// value seen or up to GROW below the largest one.  Empty: the lowest finite
+// number and 0, which needs no case of its own: a column of -inf alone ends
+// with s = 0.
 struct Stat {
     float m, s;
 };
-
-__device__ __forceinline__ Stat stat_empty() { return {-INFINITY, 0.f}; }
-
-// exp(x - m) with the maximum -inf of a column that holds nothing else read as 0.
-__device__ __forceinline__ float exp_from(float x, float m) {
-    return __expf(x - (m == -INFINITY ? 0.f : m));
-}
+constexpr float GROW = 4.f;
 
 __device__ __forceinline__ Stat stat_join(Stat a, Stat b) {
     const float m = fmaxf(a.m, b.m);
-    return {m, a.s * exp_from(a.m, m) + b.s * exp_from(b.m, m)};
+    return {m, a.s * __expf(a.m - m) + b.s * __expf(b.m - m)};
 }
 
-// stat[t][b]: 64 columns to a work-group, four rows at a time.
-template <typename TS>
-__global__ __launch_bounds__(256) void stat_kernel(LossArgs a, Stat *stat) {
-    __shared__ Stat part[4][64];
-    const int groups = (a.B + 63) / 64;
-    const int t = blockIdx.x / groups, b = (blockIdx.x % groups) * 64 + (threadIdx.x & 63);
-    const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
-    const TS *x = (const TS *)a.logits + (long)t * a.V * a.B;
-    Stat q = stat_empty();
-    if (b < a.B)
-        for (int v = row; v < a.V; v += 4)
-            q = stat_join(q, {st<TS>::load(x, (long)v * a.B + b), 1.f});
-    part[row][lane] = q;
-    __syncthreads();
-    if (row == 0 && b < a.B) {
-        for (int r = 1; r < 4; ++r)
-            q = stat_join(q, part[r][lane]);
-        stat[(long)t * a.B + b] = q;
+// U rows of VEC columns into the columns' running (m, s).  The reference
+// moves only when some value is GROW above it (the sums then rescale), so the
+// usual group costs one exponential for each element and none besides.
+template <int U, int VEC>
+__device__ __forceinline__ void stat_add(const float (*x)[VEC], float *m, float *s) {
+    float mx[VEC];
+    bool grow = false;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        mx[k] = x[0][k];
+#pragma unroll
+        for (int u = 1; u < U; ++u)
+            mx[k] = fmaxf(mx[k], x[u][k]);
+        grow |= mx[k] - m[k] > GROW;
+    }
+    if (__any(grow))
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            const float top = fmaxf(m[k], mx[k]);
+            s[k] *= __expf(m[k] - top);
+            m[k] = top;
+        }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        float sum = __expf(x[0][k] - m[k]);
+#pragma unroll
+        for (int u = 1; u < U; ++u)
+            sum += __expf(x[u][k] - m[k]);
+        s[k] += sum;
     }
 }
 
-// Per token: logp, the loss term, and what the gradient kernel multiplies by:
-// coef[n] = {m, dlogp / s, dlogp}; part[block] = the block's loss, in order.
-struct Coef {
-    float m, p, g;
+// How the logits are cut.  FLAT (columns of a row fit the work-group):
+// `lanes` threads, a multiple of the vectors after which columns repeat, walk
+// a chunk's elements in one piece.  WIDE: a wave takes 64 * VEC columns of a
+// row, the work-group's four waves every fourth row.
+struct Cut {
+    int T, V, B;
+    int rows, chunks;  // rows of a chunk, chunks of a step
+    int lanes;         // FLAT: threads at work; WIDE: 0
+    int windows;       // WIDE: windows of 64 * VEC columns
+    int mis;           // elements from the 16-byte boundary before the logits to their start
 };
 
-__global__ __launch_bounds__(256) void token_kernel(LossArgs a, const Stat *stat, Coef *coef, double *part) {
-    __shared__ double red[256];
-    const long N = (long)a.T * a.B, n = blockIdx.x * 256L + threadIdx.x;
-    double term = 0.0;
-    if (n < N) {
-        const Stat q = stat[n];
-        const int y = a.targets[n];
-        const double w = a.weights ? (double)a.weights[n] : 1.0;
-        double lp = 0.0, g = 0.0;
-        if ((uint32_t)y < (uint32_t)a.V && w != 0.0) {
-            const int t = (int)(n / a.B);
-            const long at = ((long)t * a.V + y) * a.B + (n - (long)t * a.B);
-            const float x = a.bf16 ? st<bf16_t>::load((const bf16_t *)a.logits, at) : ((const float *)a.logits)[at];
-            lp = ((double)x - (double)q.m) - log((double)q.s);
-            if (a.mode == LOSS_XENT) {
-                term = -lp;
-                g = -1.0;
-            } else if (a.mode == LOSS_POLICY) {
-                const double A = a.adv[n];
-                const double r = a.old_logp ? exp(lp - (double)a.old_logp[n]) : 1.0;
-                const double c = fmin(fmax(r, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high);
-                const double gain = r * A, held = c * A;
-                term = -(gain <= held || gain != gain ? gain : held);
-                g = gain <= held || gain != gain ? -gain : 0.0;
-                if (a.ref_logp) {
-                    const double d = (double)a.ref_logp[n] - lp, e = expm1(d);
-                    term += (double)a.kl * (e - d);
-                    g -= (double)a.kl * e;
+// A chunk's place: elements [lo, hi) counted from the 16-byte boundary.
+struct Piece {
+    int t, c, v0, v1;
+    long lo, hi;
+};
+
+__device__ __forceinline__ Piece piece_of(const Cut &g, long block) {
+    Piece p;
+    p.t = (int)(block / g.chunks);
+    p.c = (int)(block - (long)p.t * g.chunks);
+    p.v0 = p.c * g.rows;
+    p.v1 = min(g.V, p.v0 + g.rows);
+    const long s0 = (long)p.t * g.V * g.B + g.mis;
+    p.lo = s0 + (long)p.v0 * g.B;
+    p.hi = s0 + (long)p.v1 * g.B;
+    return p;
+}
+
+// The column of element `at` (counted as in Piece, not before lo - VEC).
+__device__ __forceinline__ int column_of(const Cut &g, const Piece &p, long at) {
+    const long r = at - p.lo;
+    return (int)((r + (long)g.B * 16) % g.B);
+}
+
+// VEC elements at `at`, those outside [lo, hi) -inf and not touched.
+template <typename TS, int VEC>
+__device__ __forceinline__ void load_edge(const TS *x, long at, long lo, long hi, float *f) {
+    if (at >= lo && at + VEC <= hi)
+        return vec<TS, VEC>::load(x + at, f);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+        f[k] = at + k >= lo && at + k < hi ? st<TS>::load(x, at + k) : -INFINITY;
+}
+
+template <typename TS, int VEC>
+__global__ __launch_bounds__(NT) void stat_flat_kernel(Cut g, const TS *logits, Stat *stat) {
+    constexpr int U = 4;
+    __shared__ Stat part[NT * VEC];
+    const Piece p = piece_of(g, blockIdx.x);
+    const TS *x = logits - g.mis;
+    const long first = p.lo / VEC * VEC;
+    const int j = threadIdx.x;
+    if (j < g.lanes) {
+        const long step = (long)g.lanes * VEC;
+        float m[VEC], s[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            m[k] = -FLT_MAX;
+            s[k] = 0.f;
+        }
+        long at = first + (long)j * VEC;
+        float f[U][VEC];
+        if (VEC > 1 && at < p.lo) {
+            load_edge<TS, VEC>(x, at, p.lo, p.hi, f[0]);
+            stat_add<1, VEC>(f, m, s);
+            at += step;
+        }
+        for (; at + (U - 1) * step + VEC <= p.hi; at += U * step) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                vec<TS, VEC>::load(x + at + u * step, f[u]);
+            stat_add<U, VEC>(f, m, s);
+        }
+        for (; at < p.hi; at += step) {
+            load_edge<TS, VEC>(x, at, p.lo, p.hi, f[0]);
+            stat_add<1, VEC>(f, m, s);
+        }
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+            part[j * VEC + k] = {m[k], s[k]};
+    }
+    __syncthreads();
+    // entry q is of column (c0 + q) mod B; `reps` entries of each, joined by `helpers` threads
+    const int c0 = column_of(g, p, first), reps = g.lanes * VEC / g.B;
+    const int helpers = max(1, min(reps, (int)blockDim.x / g.B));
+    for (int b = j; b < g.B * helpers; b += blockDim.x) {
+        const int h = b / g.B, q0 = (b - h * g.B + g.B - c0) % g.B;
+        Stat a = part[q0 + h * g.B];
+        for (int i = h + helpers; i < reps; i += helpers)
+            a = stat_join(a, part[q0 + i * g.B]);
+        part[q0 + h * g.B] = a;
+    }
+    __syncthreads();
+    for (int b = j; b < g.B; b += blockDim.x) {
+        const int q0 = (b + g.B - c0) % g.B;
+        Stat a = part[q0];
+        for (int h = 1; h < helpers; ++h)
+            a = stat_join(a, part[q0 + h * g.B]);
+        stat[((long)p.t * g.chunks + p.c) * g.B + b] = a;
+    }
+}
+
+template <typename TS, int VEC>
+__global__ __launch_bounds__(NT) void stat_wide_kernel(Cut g, const TS *logits, Stat *stat) {
+    constexpr int U = 4;
+    __shared__ Stat part[NT * VEC];
+    const Piece p = piece_of(g, blockIdx.x / g.windows);
+    const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
+    const long b = ((long)(blockIdx.x % g.windows) * 64 + lane) * VEC;
+    float m[VEC], s[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        m[k] = -FLT_MAX;
+        s[k] = 0.f;
+    }
+    if (b < g.B) {
+        const TS *x = logits + (long)p.t * g.V * g.B + b;
+        float f[U][VEC];
+        int v = p.v0 + row;
+        for (; v + (U - 1) * 4 < p.v1; v += U * 4) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                vec<TS, VEC>::load(x + (long)(v + u * 4) * g.B, f[u]);
+            stat_add<U, VEC>(f, m, s);
+        }
+        for (; v < p.v1; v += 4) {
+            vec<TS, VEC>::load(x + (long)v * g.B, f[0]);
+            stat_add<1, VEC>(f, m, s);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+        part[(row * VEC + k) * 64 + lane] = {m[k], s[k]};
+    __syncthreads();
+    if (row == 0 && b < g.B)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            Stat a = part[k * 64 + lane];
+            for (int r = 1; r < 4; ++r)
+                a = stat_join(a, part[(r * VEC + k) * 64 + lane]);
+            stat[((long)p.t * g.chunks + p.c) * g.B + b + k] = a;
+        }
+}
+
+// What the gradient kernel needs of a token: dL/dx_v = p * exp(min(x_v - lse, 1)),
+// p = -dlogp (with what rounding lse to fp32 left out), and the gradient at
+// the target itself.  A token that takes no part has p = 0: the minimum makes
+// its exponentials finite whatever its logits are, so it gets zeros.
+struct Coef {
+    float lse, p;
+};
+
+// Four threads join a token's chunks; one of them does its terms in fp64.
+__global__ __launch_bounds__(NT) void token_kernel(LossArgs a, int chunks, const Stat *stat, Coef *coef, float *dtarget,
+                                                   double *part) {
+    __shared__ Stat join[4][64];
+    __shared__ double red[64];
+    const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
+    const long N = (long)a.T * a.B, n = blockIdx.x * 64L + lane;
+    const int t = (int)(n / a.B), b = (int)(n - (long)t * a.B);
+    Stat q = {-FLT_MAX, 0.f};
+    if (n < N)
+        for (int c = row; c < chunks; c += 4)
+            q = stat_join(q, stat[((long)t * chunks + c) * a.B + b]);
+    join[row][lane] = q;
+    __syncthreads();
+    if (row == 0) {
+        double term = 0.0;
+        if (n < N) {
+            for (int r = 1; r < 4; ++r)
+                q = stat_join(q, join[r][lane]);
+            const int y = a.targets[n];
+            const double w = a.weights ? (double)a.weights[n] : 1.0;
+            double lp = 0.0, g = 0.0;
+            Coef c = {0.f, 0.f};
+            float dt = 0.f;
+            if ((uint32_t)y < (uint32_t)a.V && w != 0.0) {
+                const long at = ((long)t * a.V + y) * a.B + b;
+                const float x = a.bf16 ? st<bf16_t>::load((const bf16_t *)a.logits, at) : ((const float *)a.logits)[at];
+                const double ls = log((double)q.s), lse = (double)q.m + ls;
+                lp = ((double)x - (double)q.m) - ls;
+                if (a.mode == LOSS_XENT) {
+                    term = -lp;
+                    g = -1.0;
+                } else if (a.mode == LOSS_POLICY) {
+                    const double A = a.adv[n];
+                    const double r = a.old_logp ? exp(lp - (double)a.old_logp[n]) : 1.0;
+                    const double cl = fmin(fmax(r, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high);
+                    const double gain = r * A, held = cl * A;
+                    const bool open = gain <= held || gain != gain;
+                    term = -(open ? gain : held);
+                    g = open ? -gain : 0.0;
+                    if (a.ref_logp) {
+                        const double d = (double)a.ref_logp[n] - lp, e = expm1(d);
+                        term += (double)a.kl * (e - d);
+                        g -= (double)a.kl * e;
+                    }
+                }
+                term *= w * (double)a.scale;
+                g *= w * (double)a.scale;
+                if (g != 0.0) {
+                    c.lse = (float)lse;
+                    c.p = (float)(-g * exp((double)c.lse - lse));
+                    dt = (float)(-g * expm1(lp));
                 }
             }
-            term *= w * (double)a.scale;
-            g *= w * (double)a.scale;
+            if (a.logp)
+                a.logp[n] = (float)lp;
+            coef[n] = c;
+            dtarget[n] = dt;
         }
-        if (a.logp)
-            a.logp[n] = (float)lp;
-        coef[n] = {q.m, (float)(g / (double)q.s), (float)g};
+        red[lane] = term;
     }
-    red[threadIdx.x] = term;
     __syncthreads();
-    for (int w = 128; w >= 1; w >>= 1) {
+    for (int w = 32; w >= 1; w >>= 1) {
         if ((int)threadIdx.x < w)
             red[threadIdx.x] += red[threadIdx.x + w];
         __syncthreads();
@@ -104,14 +295,15 @@ __global__ __launch_bounds__(256) void token_kernel(LossArgs a, const Stat *stat
         part[blockIdx.x] = red[0];
 }
 
-__global__ __launch_bounds__(256) void loss_sum_kernel(const double *part, int n, float *loss) {
-    __shared__ double red[256];
+// The token kernel's partial sums in a fixed order.
+__global__ __launch_bounds__(NT) void loss_sum_kernel(const double *part, int n, float *loss) {
+    __shared__ double red[NT];
     double sum = 0.0;
-    for (int i = threadIdx.x; i < n; i += 256)
+    for (int i = threadIdx.x; i < n; i += NT)
         sum += part[i];
     red[threadIdx.x] = sum;
     __syncthreads();
-    for (int w = 128; w >= 1; w >>= 1) {
+    for (int w = NT / 2; w >= 1; w >>= 1) {
         if ((int)threadIdx.x < w)
             red[threadIdx.x] += red[threadIdx.x + w];
         __syncthreads();
@@ -120,86 +312,221 @@ __global__ __launch_bounds__(256) void loss_sum_kernel(const double *part, int n
         *loss = (float)red[0];
 }
 
+__device__ __forceinline__ float grad_of(float x, Coef c) { return c.p * __expf(fminf(x - c.lse, 1.f)); }
+
+// The targets' own elements of a piece, written over what the softmax's term
+// alone gave them (same work-group, after a barrier).
 template <typename TS>
-__global__ __launch_bounds__(256) void grad_kernel(LossArgs a, const Coef *coef) {
-    const long n = (long)a.T * a.V * a.B;
-    const TS *x = (const TS *)a.logits;
-    TS *y = (TS *)a.dlogits;
-    for (long e = blockIdx.x * 256L + threadIdx.x; e < n; e += (long)gridDim.x * 256) {
-        const long tv = e / a.B;
-        const int b = (int)(e - tv * a.B), t = (int)(tv / a.V), v = (int)(tv - (long)t * a.V);
-        const long k = (long)t * a.B + b;
-        const Coef c = coef[k];
-        float d = 0.f;
-        if (c.g != 0.f) {
-            d = -c.p * exp_from(st<TS>::load(x, e), c.m);
-            if (a.targets[k] == v)
-                d += c.g;
-        }
-        st<TS>::store(y, e, d);
+__device__ __forceinline__ void grad_targets(const Cut &g, const Piece &p, int b0, int b1, const int32_t *targets,
+                                             const float *dtarget, TS *y) {
+    for (int b = b0 + threadIdx.x; b < b1; b += blockDim.x) {
+        const long n = (long)p.t * g.B + b;
+        const int v = targets[n];
+        if (v >= p.v0 && v < p.v1)
+            st<TS>::store(y, ((long)p.t * g.V + v) * g.B + b, dtarget[n]);
     }
+}
+
+template <typename TS, int VEC>
+__global__ __launch_bounds__(NT) void grad_flat_kernel(Cut g, const TS *logits, TS *dlogits, const int32_t *targets,
+                                                       const Coef *coef, const float *dtarget) {
+    constexpr int U = 4;
+    const Piece p = piece_of(g, blockIdx.x);
+    const TS *x = logits - g.mis;
+    TS *y = dlogits - g.mis;
+    const long first = p.lo / VEC * VEC;
+    const int j = threadIdx.x;
+    if (j < g.lanes) {
+        const long step = (long)g.lanes * VEC;
+        long at = first + (long)j * VEC;
+        Coef c[VEC];
+        int b = column_of(g, p, at);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            c[k] = coef[(long)p.t * g.B + b];
+            b = b + 1 == g.B ? 0 : b + 1;
+        }
+        float f[U][VEC];
+        auto edge = [&] {
+            load_edge<TS, VEC>(x, at, p.lo, p.hi, f[0]);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k)
+                f[0][k] = grad_of(f[0][k], c[k]);
+            if (at >= p.lo && at + VEC <= p.hi) {
+                vec<TS, VEC>::store(y + at, f[0]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < VEC; ++k)
+                    if (at + k >= p.lo && at + k < p.hi)
+                        st<TS>::store(y, at + k, f[0][k]);
+            }
+            at += step;
+        };
+        if (VEC > 1 && at < p.lo)
+            edge();
+        for (; at + (U - 1) * step + VEC <= p.hi; at += U * step) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                vec<TS, VEC>::load(x + at + u * step, f[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int k = 0; k < VEC; ++k)
+                    f[u][k] = grad_of(f[u][k], c[k]);
+                vec<TS, VEC>::store(y + at + u * step, f[u]);
+            }
+        }
+        while (at < p.hi)
+            edge();
+    }
+    __syncthreads();
+    grad_targets(g, p, 0, g.B, targets, dtarget, dlogits);
+}
+
+template <typename TS, int VEC>
+__global__ __launch_bounds__(NT) void grad_wide_kernel(Cut g, const TS *logits, TS *dlogits, const int32_t *targets,
+                                                       const Coef *coef, const float *dtarget) {
+    constexpr int U = 4;
+    const Piece p = piece_of(g, blockIdx.x / g.windows);
+    const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
+    const int w0 = (int)(blockIdx.x % g.windows) * 64 * VEC, b = w0 + lane * VEC;
+    if (b < g.B) {
+        Coef c[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+            c[k] = coef[(long)p.t * g.B + b + k];
+        const long s0 = (long)p.t * g.V * g.B + b;
+        float f[U][VEC];
+        int v = p.v0 + row;
+        for (; v + (U - 1) * 4 < p.v1; v += U * 4) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                vec<TS, VEC>::load(logits + s0 + (long)(v + u * 4) * g.B, f[u]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int k = 0; k < VEC; ++k)
+                    f[u][k] = grad_of(f[u][k], c[k]);
+                vec<TS, VEC>::store(dlogits + s0 + (long)(v + u * 4) * g.B, f[u]);
+            }
+        }
+        for (; v < p.v1; v += 4) {
+            vec<TS, VEC>::load(logits + s0 + (long)v * g.B, f[0]);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k)
+                f[0][k] = grad_of(f[0][k], c[k]);
+            vec<TS, VEC>::store(dlogits + s0 + (long)v * g.B, f[0]);
+        }
+    }
+    __syncthreads();
+    grad_targets(g, p, w0, min(g.B, w0 + 64 * VEC), targets, dtarget, dlogits);
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// A work-group's share of a step: `bytes` or more of logits, and no more
+// groups than `groups` over all steps.
+constexpr long GROUPS = 2048, BYTES = 16384;
+
+// The cut for vectors of VEC elements.
+Cut cut_of(int T, int B, int V, int es, int VEC, int mis) {
+    Cut g = {T, V, B, V, 1, 0, 1, mis};
+    const int repeat = B / std::gcd(B, VEC);
+    if (repeat <= NT)
+        g.lanes = NT / repeat * repeat;
+    else
+        g.windows = (int)ceil_div(B, 64 * VEC);
+    const long across = (long)T * g.windows;
+    const long by_groups = ceil_div(GROUPS, across), by_bytes = (long)V * B * es / g.windows / BYTES;
+    long chunks = std::max(1L, std::min(std::min(by_groups, by_bytes), (long)V));
+    g.rows = (int)ceil_div(V, chunks);
+    g.chunks = (int)ceil_div(V, g.rows);
+    return g;
+}
+
 struct LossWs {
     Stat *stat;
     Coef *coef;
+    float *dtarget;
     double *part;
     size_t bytes;
     int parts;
 };
 
-LossWs layout(void *ws, int T, int B) {
+LossWs layout(void *ws, int T, int B, size_t chunks) {
     const size_t N = (size_t)T * B;
     char *p = (char *)ws;
     LossWs w;
-    w.parts = (int)((N + 255) / 256);
+    w.parts = (int)((N + 63) / 64);
     size_t at = 0;
     w.stat = (Stat *)(p + at);
-    at += align256(N * sizeof(Stat));
+    at += align256(N * chunks * sizeof(Stat));
     w.coef = (Coef *)(p + at);
     at += align256(N * sizeof(Coef));
+    w.dtarget = (float *)(p + at);
+    at += align256(N * sizeof(float));
     w.part = (double *)(p + at);
     at += align256((size_t)w.parts * 8);
     w.bytes = at;
     return w;
 }
 
-} // namespace
-
-size_t loss_ws(int T, int B, int V, bool bf16) {
-    (void)V;
-    (void)bf16;
-    return layout(nullptr, T, B).bytes;
-}
-
-hipError_t launch_loss(const LossArgs &a, hipStream_t s) {
-    const LossWs w = layout(a.ws, a.T, a.B);
+template <typename TS, int VEC>
+hipError_t run(const LossArgs &a, Cut g, const LossWs &w, hipStream_t s) {
+    const TS *x = (const TS *)a.logits;
+    TS *y = (TS *)a.dlogits;
     hipError_t e;
-    const dim3 blk(256), gs((unsigned)((long)a.T * ceil_div(a.B, 64)));
-    if (a.bf16)
-        hipLaunchKernelGGL(stat_kernel<bf16_t>, gs, blk, 0, s, a, w.stat);
+    const unsigned grid = (unsigned)((long)g.T * g.chunks * g.windows);
+    const unsigned flat = (unsigned)(ceil_div(std::max(g.lanes, 1), 64) * 64);
+    if (g.lanes)
+        hipLaunchKernelGGL((stat_flat_kernel<TS, VEC>), dim3(grid), dim3(flat), 0, s, g, x, w.stat);
     else
-        hipLaunchKernelGGL(stat_kernel<float>, gs, blk, 0, s, a, w.stat);
+        hipLaunchKernelGGL((stat_wide_kernel<TS, VEC>), dim3(grid), dim3(NT), 0, s, g, x, w.stat);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
-    hipLaunchKernelGGL(token_kernel, dim3((unsigned)w.parts), blk, 0, s, a, w.stat, w.coef, w.part);
+    hipLaunchKernelGGL(token_kernel, dim3((unsigned)w.parts), dim3(NT), 0, s, a, g.chunks, w.stat, w.coef, w.dtarget,
+                       w.part);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
     if (a.loss) {
-        hipLaunchKernelGGL(loss_sum_kernel, dim3(1), blk, 0, s, w.part, w.parts, a.loss);
+        hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(NT), 0, s, w.part, w.parts, a.loss);
         if ((e = hipGetLastError()) != hipSuccess)
             return e;
     }
-    if (!a.dlogits)
+    if (!y)
         return hipSuccess;
-    const dim3 gg((unsigned)std::min(ceil_div((long)a.T * a.V * a.B, 256L), 16384L));
-    if (a.bf16)
-        hipLaunchKernelGGL(grad_kernel<bf16_t>, gg, blk, 0, s, a, w.coef);
+    if (g.lanes)
+        hipLaunchKernelGGL((grad_flat_kernel<TS, VEC>), dim3(grid), dim3(flat), 0, s, g, x, y, a.targets, w.coef, w.dtarget);
     else
-        hipLaunchKernelGGL(grad_kernel<float>, gg, blk, 0, s, a, w.coef);
+        hipLaunchKernelGGL((grad_wide_kernel<TS, VEC>), dim3(grid), dim3(NT), 0, s, g, x, y, a.targets, w.coef, w.dtarget);
     return hipGetLastError();
+}
+
+// Vectors where the logits and their gradient lie alike to the 16 bytes and,
+// for rows wider than a work-group, every row does; else single elements.
+template <typename TS>
+hipError_t dispatch(const LossArgs &a, hipStream_t s) {
+    constexpr int VEC = vec_of<TS>(), ES = st<TS>::bytes;
+    const int mis = (int)((uintptr_t)a.logits / ES % VEC);
+    const bool alike = !a.dlogits || (int)((uintptr_t)a.dlogits / ES % VEC) == mis;
+    Cut g = cut_of(a.T, a.B, a.V, ES, VEC, mis);
+    if (alike && (g.lanes || (mis == 0 && a.B % VEC == 0)))
+        return run<TS, VEC>(a, g, layout(a.ws, a.T, a.B, g.chunks), s);
+    g = cut_of(a.T, a.B, a.V, ES, 1, 0);
+    return run<TS, 1>(a, g, layout(a.ws, a.T, a.B, g.chunks), s);
+}
+
+} // namespace
+
+// For either cut: where the tensors start is not known here.
+size_t loss_ws(int T, int B, int V, bool bf16) {
+    const int es = bf16 ? 2 : 4;
+    const int a = cut_of(T, B, V, es, 16 / es, 0).chunks, b = cut_of(T, B, V, es, 1, 0).chunks;
+    return layout(nullptr, T, B, (size_t)std::max(a, b)).bytes;
+}
+
+hipError_t launch_loss(const LossArgs &a, hipStream_t s) {
+    return a.bf16 ? dispatch<bf16_t>(a, s) : dispatch<float>(a, s);
 }
 
 } // namespace lstmss
