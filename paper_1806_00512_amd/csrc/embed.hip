@@ -1,108 +1,486 @@
-// Embedding lookup into the batch-last layout, and its gradient by sorted tokens.
+// Embedding lookup into the batch-last layout, and its gradient by sorted
+// tokens.
+//
+// Lookup: x[t][i][b] = scale * E[tokens[t][b]][i].  The table has its features
+// in one piece, x its batch: a work-group reads 64 features of up to 64
+// columns' rows, turns them over in LDS and writes them batch-last.
+//
+// Gradient: dE[v][i] = scale * sum of dX[t][i][b] over the (t, b) with token v.
+//   sort_kernel   the positions' ranks by (token, position), and each token's
+//                 range of ranks
+//   turn_kernel   dX turned over as in the lookup, each position's row written
+//                 at its rank (the row of a token that stands once goes straight
+//                 into dE); rows of tokens that do not occur are zeroed by the
+//                 same launch
+//   walk_kernel   sums of equal tokens' rows, which now follow one another, over
+//                 groups of rows
+//   carry_kernel  tokens whose rows lie in several groups
+// The order of every sum follows from the tokens alone.
 #include <algorithm>
 
 #include "common.h"
 #include "language.h"
 #include "philox.h"
+#include "vec.h"
 
 namespace lstmss {
 
 namespace {
 
-// x[t][i][b] = scale * E[tokens[t][b]][i]: one thread for each element.
-template <typename TS>
-__global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a) {
-    const long n = (long)a.T * a.I * a.B;
-    const TS *E = (const TS *)a.E;
-    for (long e = blockIdx.x * 256L + threadIdx.x; e < n; e += (long)gridDim.x * 256) {
-        const long ti = e / a.B;
-        const int b = (int)(e - ti * a.B);
-        const int t = (int)(ti / a.I), i = (int)(ti - (long)t * a.I);
-        const int32_t v = a.tokens[(long)t * a.B + b];
-        const float f = (uint32_t)v < (uint32_t)a.V ? st<TS>::load(E, (long)v * a.I + i) * a.scale : 0.f;
-        st<TS>::store((TS *)a.x, e, drop_one(a.drop, e, f));
-    }
+constexpr int NT = 256;
+constexpr int TILE = 64;        // features and columns of a tile
+constexpr int PITCH = TILE + 1; // its columns' distance in LDS: both ways of access meet all banks alike
+
+// A step's columns are cut into chunks of `cols` (one chunk: cols = B), its
+// features into tiles of 64.  With one chunk a tile of the batch-last tensor
+// is one piece of memory, else it is a piece for each feature.
+struct Tiling {
+    int T, B, I;
+    int cols, chunks, tiles;
+};
+
+struct Tile {
+    int t, b0, nb, i0, ni;
+};
+
+__device__ __forceinline__ Tile tile_of(const Tiling &g, long block) {
+    Tile a;
+    const long tc = block / g.tiles;
+    a.i0 = (int)(block - tc * g.tiles) * TILE;
+    a.t = (int)(tc / g.chunks);
+    a.b0 = (int)(tc - (long)a.t * g.chunks) * g.cols;
+    a.nb = min(g.cols, g.B - a.b0);
+    a.ni = min(TILE, g.I - a.i0);
+    return a;
 }
 
-// order[r] = the position whose (token, position) has rank r: each position
-// counts those before it.  Tokens outside [0, V) come last, as V.
-__global__ __launch_bounds__(256) void rank_kernel(const int32_t *tokens, int N, int V, int32_t *key,
-                                                   int32_t *order) {
-    const int p = blockIdx.x * 256 + threadIdx.x;
-    if (p >= N)
-        return;
-    const uint32_t mine = min((uint32_t)tokens[p], (uint32_t)V);
-    int r = 0;
-    for (int q = 0; q < N; ++q) {
-        const uint32_t other = min((uint32_t)tokens[q], (uint32_t)V);
-        r += other < mine || (other == mine && q < p);
-    }
-    key[r] = (int32_t)mine;
-    order[r] = p;
-}
-
-// First r with key[r] >= v.
-__device__ __forceinline__ int lower_bound(const int32_t *key, int N, int v) {
-    int lo = 0, hi = N;
-    while (lo < hi) {
-        const int mid = lo + (hi - lo) / 2;
-        if (key[mid] < v)
-            lo = mid + 1;
-        else
-            hi = mid;
-    }
-    return lo;
-}
-
-// dE[v][i]: one work-group for each row, summing its positions in order.
-__global__ __launch_bounds__(256) void embed_grad_kernel(EmbedGradArgs a, int N, const int32_t *key,
-                                                         const int32_t *order) {
-    const int v = blockIdx.x;
-    const int r0 = lower_bound(key, N, v), r1 = lower_bound(key, N, v + 1);
-    if (a.accumulate && r0 == r1)
-        return;
-    for (int i = threadIdx.x; i < a.I; i += 256) {
-        float sum = 0.f;
-        for (int r = r0; r < r1; ++r) {
-            const int t = order[r] / a.B, b = order[r] - t * a.B;
-            const long e = ((long)t * a.I + i) * a.B + b;
-            sum += drop_one(a.drop, e, a.dX[e]);
+// Calls f(e, lo, hi, i, b) for the groups of eight elements e .. e + 7 (e a
+// multiple of 8) that cover a tile of the batch-last tensor, those in [lo, hi)
+// its own: element e + k is of column b + k, feature i while b + k < B, of the
+// next features from there.  b may be negative down to -7 in a group that
+// begins before its piece.
+template <class F>
+__device__ __forceinline__ void for_groups(const Tiling &g, const Tile &a, F &&f) {
+    if (g.chunks == 1) {
+        const long lo = ((long)a.t * g.I + a.i0) * g.B, hi = lo + (long)a.ni * g.B;
+        const long q0 = lo >> 3, q1 = (hi + 7) >> 3;
+        for (long q = q0 + threadIdx.x; q < q1; q += NT) {
+            const int r = (int)(q * 8 - lo);
+            const int i = r < 0 ? 0 : r / g.B;
+            f(q * 8, lo, hi, i, r - i * g.B);
         }
-        float *p = a.dE + (long)v * a.I + i;
-        *p = a.accumulate ? *p + sum * a.scale : sum * a.scale;
+    } else {
+        const int per = (a.nb + 7) / 8 + 1;
+        for (int n = threadIdx.x; n < per * a.ni; n += NT) {
+            const int i = n / per, j = n - i * per;
+            const long lo = ((long)a.t * g.I + a.i0 + i) * g.B + a.b0, hi = lo + a.nb;
+            const long e = (lo >> 3) * 8 + j * 8;
+            if (e < hi)
+                f(e, lo, hi, i, (int)(e - lo));
+        }
     }
+}
+
+template <typename TS, int LV>
+__global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, bool aligned) {
+    __shared__ float tile[TILE * PITCH];
+    __shared__ int row[TILE];
+    const Tile w = tile_of(g, blockIdx.x);
+    if ((int)threadIdx.x < w.nb) {
+        const int v = a.tokens[(long)w.t * g.B + w.b0 + threadIdx.x];
+        row[threadIdx.x] = (uint32_t)v < (uint32_t)a.V ? v : -1;
+    }
+    __syncthreads();
+    constexpr int PER = TILE / LV;
+    const TS *E = (const TS *)a.E;
+    for (int n = threadIdx.x; n < w.nb * PER; n += NT) {
+        const int b = n / PER, i = (n - b * PER) * LV;
+        float f[LV] = {};
+        if (row[b] >= 0 && i < w.ni)
+            vec<TS, LV>::load(E + (long)row[b] * g.I + w.i0 + i, f);
+#pragma unroll
+        for (int k = 0; k < LV; ++k)
+            tile[b * PITCH + i + k] = f[k];
+    }
+    __syncthreads();
+    TS *x = (TS *)a.x;
+    for_groups(g, w, [&](long e, long lo, long hi, int i, int b) {
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const bool in = e + k >= lo && e + k < hi;
+            f[k] = in ? tile[b * PITCH + i] * a.scale : 0.f;
+            if (++b == g.B) {
+                b = 0;
+                ++i;
+            }
+        }
+        drop8(a.drop, e, f);
+        if (aligned && e >= lo && e + 8 <= hi)
+            return store8(x + e, f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (e + k >= lo && e + k < hi)
+                st<TS>::store(x, e + k, f[k]);
+    });
+}
+
+// ------------------------------------------------------------ gradient
+
+constexpr int SORT_NT = 1024, SORT_WAVES = SORT_NT / 64, SORT_MOST = 512;
+
+// Work-group w places the tokens [w R, (w + 1) R): every wave counts its share
+// of the positions by token; the counts before a (wave, token), with those of
+// all smaller tokens, are where that wave's first position of the token goes,
+// and the waves then go over their shares again in order.  Every work-group
+// reads all tokens, which lie in the caches; none waits for another.
+__global__ __launch_bounds__(SORT_NT) void sort_kernel(const int32_t *tokens, int N, int V, int R, int32_t *rank,
+                                                       int32_t *key, int32_t *start) {
+    __shared__ int hist[SORT_WAVES][SORT_MOST];
+    __shared__ int less[SORT_WAVES], sums[SORT_WAVES];
+    const int lo = blockIdx.x * R, n = min(V - lo, R);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    for (int k = lane; k < R; k += 64)
+        hist[w][k] = 0;
+    __syncthreads();
+    const int share = (int)(ceil_div(N, SORT_NT) * 64);
+    const int p0 = (int)min((long)N, (long)w * share), p1 = (int)min((long)N, (long)p0 + share);
+    int before = 0;
+    for (int p = p0 + lane; p < p1; p += 64) {
+        const uint32_t v = (uint32_t)tokens[p];
+        before += v < (uint32_t)lo;
+        if (v - (uint32_t)lo < (uint32_t)n)
+            atomicAdd(&hist[w][v - lo], 1);
+    }
+    for (int m = 32; m >= 1; m >>= 1)
+        before += __shfl_xor(before, m, 64);
+    if (lane == 0)
+        less[w] = before;
+    __syncthreads();
+    int at = 0;
+    for (int k = 0; k < SORT_WAVES; ++k)
+        at += less[k];
+    // exclusive sums over the tokens (one for each of the first 512 threads), then over the waves
+    int total = 0;
+    if ((int)threadIdx.x < n)
+        for (int k = 0; k < SORT_WAVES; ++k)
+            total += hist[k][threadIdx.x];
+    int sum = total;
+    for (int m = 1; m < 64; m <<= 1) {
+        const int o = __shfl_up(sum, m, 64);
+        sum += lane >= m ? o : 0;
+    }
+    if (lane == 63)
+        sums[w] = sum;
+    __syncthreads();
+    for (int k = 0; k < w; ++k)
+        sum += sums[k];
+    if ((int)threadIdx.x < n) {
+        int first = at + sum - total;
+        start[lo + threadIdx.x] = first;
+        if (lo + (int)threadIdx.x == V - 1)
+            start[V] = first + total;
+        for (int k = 0; k < SORT_WAVES; ++k) {
+            const int c = hist[k][threadIdx.x];
+            hist[k][threadIdx.x] = first;
+            first += c;
+        }
+    }
+    __syncthreads();
+    volatile int *next = hist[w];
+    for (int base = p0; base < p1; base += 64) {
+        const int p = base + lane;
+        const int v = p < p1 ? tokens[p] : -1;
+        const bool in = (uint32_t)v - (uint32_t)lo < (uint32_t)n;
+        for (uint64_t left = __ballot(in); left;) {
+            const int l = __ffsll((long long)left) - 1;
+            const int token = __shfl(v, l, 64);
+            const uint64_t same = __ballot(in && v == token);
+            const int first = next[token - lo];
+            if (in && v == token) {
+                const int r = first + __popcll(same & ((1ull << lane) - 1));
+                rank[p] = r;
+                key[r] = v;
+            }
+            if (lane == l)
+                next[token - lo] = first + __popcll(same);
+            left &= ~same;
+        }
+    }
+}
+
+// A token's range of ranks.
+struct Sorted {
+    const int32_t *rank, *key, *start; // [N], [N], [V + 1]
+};
+
+__device__ __forceinline__ void put(const EmbedGradArgs &a, float *p, float sum) {
+    *p = a.accumulate ? *p + sum * a.scale : sum * a.scale;
+}
+
+constexpr int ZERO_ROWS = 16; // rows of dE that a work-group looks at
+
+__device__ __forceinline__ void zero_rows(const EmbedGradArgs &a, const int32_t *start, long block, bool aligned) {
+    const int v0 = (int)(block * ZERO_ROWS), v1 = (int)min((long)a.V, (block + 1) * ZERO_ROWS);
+    for (int v = v0; v < v1; ++v) {
+        if (start[v] != start[v + 1])
+            continue;
+        float *p = a.dE + (long)v * a.I;
+        if (aligned) {
+            for (int i = threadIdx.x * 4; i < a.I; i += NT * 4)
+                *(f32x4 *)(p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
+        } else {
+            for (int i = threadIdx.x; i < a.I; i += NT)
+                p[i] = 0.f;
+        }
+    }
+}
+
+__global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sorted q, float *rows, long tiles,
+                                                  bool aligned, bool zero_aligned) {
+    __shared__ float tile[TILE * PITCH];
+    __shared__ float *dest[TILE];
+    __shared__ bool once[TILE];
+    if (blockIdx.x >= tiles)
+        return zero_rows(a, q.start, blockIdx.x - tiles, zero_aligned);
+    const Tile w = tile_of(g, blockIdx.x);
+    if ((int)threadIdx.x < w.nb) {
+        const long p = (long)w.t * g.B + w.b0 + threadIdx.x;
+        const int v = a.tokens[p];
+        float *d = nullptr;
+        bool one = false;
+        if ((uint32_t)v < (uint32_t)a.V) {
+            one = q.start[v + 1] - q.start[v] == 1;
+            d = one ? a.dE + (long)v * a.I : rows + (long)q.rank[p] * a.I;
+        }
+        dest[threadIdx.x] = d;
+        once[threadIdx.x] = one;
+    }
+    for_groups(g, w, [&](long e, long lo, long hi, int i, int b) {
+        float f[8];
+        if (aligned && e >= lo && e + 8 <= hi) {
+            load8(a.dX + e, f);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                f[k] = e + k >= lo && e + k < hi ? a.dX[e + k] : 0.f;
+        }
+        drop8(a.drop, e, f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (e + k >= lo && e + k < hi)
+                tile[b * PITCH + i] = f[k];
+            if (++b == g.B) {
+                b = 0;
+                ++i;
+            }
+        }
+    });
+    __syncthreads();
+    const int lane = threadIdx.x & 63;
+    if (lane < w.ni)
+        for (int b = threadIdx.x >> 6; b < w.nb; b += NT / 64) {
+            float *d = dest[b];
+            if (!d)
+                continue;
+            const float f = tile[b * PITCH + lane];
+            d += w.i0 + lane;
+            if (once[b])
+                put(a, d, f);
+            else
+                *d = f;
+        }
+}
+
+// Rows [G q, G q + G) of the sorted rows, VEC features to a thread: the sums
+// of runs of equal tokens.  A run that begins and ends here is finished; what
+// continues from the group before goes to carry[q][0], what begins here and
+// goes on to carry[q][1].
+template <int G, int VEC>
+__global__ __launch_bounds__(NT) void walk_kernel(EmbedGradArgs a, Sorted q, const float *rows, float *carry, int parts) {
+    constexpr int U = 8;
+    __shared__ int key[G + 2];
+    const int group = blockIdx.x / parts, part = blockIdx.x - group * parts;
+    const int M = q.start[a.V];
+    const long r0 = (long)group * G;
+    if (r0 >= M)
+        return;
+    const int n = (int)min((long)G, M - r0);
+    for (int k = threadIdx.x; k < n + 2; k += NT) {
+        const long r = r0 + k - 1;
+        key[k] = r >= 0 && r < M ? q.key[r] : -1;
+    }
+    __syncthreads();
+    const int i = (part * NT + threadIdx.x) * VEC;
+    if (i >= a.I)
+        return;
+    float sum[VEC] = {};
+    bool begun = key[0] != key[1]; // the run at hand begins in this group
+    for (int k0 = 0; k0 < n; k0 += U) {
+        float f[U][VEC];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k0 + u;
+            // a row whose token stands once is not there
+            if (k < n && (key[k] == key[k + 1] || key[k + 1] == key[k + 2]))
+                vec<float, VEC>::load(rows + (r0 + k) * a.I + i, f[u]);
+            else
+#pragma unroll
+                for (int j = 0; j < VEC; ++j)
+                    f[u][j] = 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k0 + u;
+            if (k >= n)
+                break;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                sum[j] += f[u][j];
+            const int v = key[k + 1];
+            const bool ends = v != key[k + 2];
+            if (!ends && k + 1 < n)
+                continue;
+            if (begun && ends) {
+                if (v != key[k]) {
+                    // stands once: written already
+                } else {
+                    float *p = a.dE + (long)v * a.I + i;
+                    float out[VEC] = {};
+                    if (a.accumulate)
+                        vec<float, VEC>::load(p, out);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j)
+                        out[j] = a.accumulate ? out[j] + sum[j] * a.scale : sum[j] * a.scale;
+                    vec<float, VEC>::store(p, out);
+                }
+            } else {
+                float *p = carry + ((long)group * 2 + (begun ? 1 : 0)) * a.I + i;
+                vec<float, VEC>::store(p, sum);
+            }
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                sum[j] = 0.f;
+            begun = true;
+        }
+    }
+}
+
+// The run that crosses into group q from where it begins, in group q - 1: the
+// sums of its parts, in order.
+__global__ __launch_bounds__(NT) void carry_kernel(EmbedGradArgs a, Sorted s, const float *carry, int G, int parts) {
+    const int q = blockIdx.x / parts + 1, part = blockIdx.x - (q - 1) * parts;
+    const long r = (long)q * G;
+    if (r >= s.start[a.V] || s.key[r - 1] != s.key[r])
+        return;
+    const int v = s.key[r];
+    if (s.start[v] < r - G)
+        return; // begins before group q - 1
+    const int i = part * NT + threadIdx.x;
+    if (i >= a.I)
+        return;
+    const int last = (s.start[v + 1] - 1) / G;
+    const float first = carry[((long)(q - 1) * 2 + 1) * a.I + i];
+    put(a, a.dE + (long)v * a.I + i, sum_parts(first, carry + (long)q * 2 * a.I + i, last - q + 1, 2L * a.I));
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+Tiling tiling_of(int T, int B, int I) {
+    Tiling g = {T, B, I, B, 1, (int)ceil_div(I, TILE)};
+    if (B > TILE) {
+        // whole eights, so that only odd batches have groups of two pieces
+        g.chunks = (int)ceil_div(B, TILE);
+        g.cols = (int)ceil_div(ceil_div(B, g.chunks), 8) * 8;
+        g.chunks = (int)ceil_div(B, g.cols);
+    }
+    return g;
+}
+
+// Rows of a group of the walk: more groups while there are few rows.
+int group_of(int N) { return N < 4096 ? 16 : 64; }
+
+struct GradWs {
+    int32_t *rank, *key, *start;
+    float *rows, *carry;
+    size_t bytes;
+};
+
+GradWs layout(void *ws, int N, int I, int V) {
+    char *p = (char *)ws;
+    GradWs w;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char *r = p + at;
+        at += align256(bytes);
+        return r;
+    };
+    w.rank = (int32_t *)take((size_t)N * 4);
+    w.key = (int32_t *)take((size_t)N * 4);
+    w.start = (int32_t *)take(((size_t)V + 1) * 4);
+    w.rows = (float *)take((size_t)N * I * 4);
+    w.carry = (float *)take((size_t)ceil_div(N, group_of(N)) * 2 * I * 4);
+    w.bytes = at;
+    return w;
+}
+
+template <typename TS>
+hipError_t lookup(const EmbedArgs &a, hipStream_t s) {
+    constexpr int LV = vec_of<TS>();
+    const Tiling g = tiling_of(a.T, a.B, a.I);
+    const dim3 grid((unsigned)((long)g.T * g.chunks * g.tiles));
+    const bool aligned = (uintptr_t)a.x % 16 == 0;
+    if ((uintptr_t)a.E % 16 == 0 && a.I % LV == 0)
+        hipLaunchKernelGGL((embed_kernel<TS, LV>), grid, dim3(NT), 0, s, a, g, aligned);
+    else
+        hipLaunchKernelGGL((embed_kernel<TS, 1>), grid, dim3(NT), 0, s, a, g, aligned);
+    return hipGetLastError();
+}
+
+template <int G>
+hipError_t walk(const EmbedGradArgs &a, const Sorted &q, const GradWs &w, int N, bool aligned, hipStream_t s) {
+    const int groups = (int)ceil_div(N, G);
+    const int parts = (int)ceil_div(a.I, NT * (aligned ? 4 : 1));
+    const dim3 grid((unsigned)((long)groups * parts));
+    if (aligned)
+        hipLaunchKernelGGL((walk_kernel<G, 4>), grid, dim3(NT), 0, s, a, q, w.rows, w.carry, parts);
+    else
+        hipLaunchKernelGGL((walk_kernel<G, 1>), grid, dim3(NT), 0, s, a, q, w.rows, w.carry, parts);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || groups < 2)
+        return e;
+    const int cparts = (int)ceil_div(a.I, NT);
+    hipLaunchKernelGGL(carry_kernel, dim3((unsigned)((long)(groups - 1) * cparts)), dim3(NT), 0, s, a, q, w.carry, G, cparts);
+    return hipGetLastError();
+}
+
 } // namespace
 
 hipError_t launch_embed(const EmbedArgs &a, bool bf16, hipStream_t s) {
-    const long n = (long)a.T * a.I * a.B;
-    const dim3 grid((unsigned)std::min(ceil_div(n, 256L), 8192L));
-    if (bf16)
-        hipLaunchKernelGGL(embed_kernel<bf16_t>, grid, dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL(embed_kernel<float>, grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+    return bf16 ? lookup<bf16_t>(a, s) : lookup<float>(a, s);
 }
 
-size_t embed_grad_ws(int T, int B, int I, int V) {
-    (void)I;
-    (void)V;
-    return 2 * align256((size_t)T * B * 4);
-}
+size_t embed_grad_ws(int T, int B, int I, int V) { return layout(nullptr, T * B, I, V).bytes; }
 
 hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
     const int N = a.T * a.B;
-    int32_t *key = (int32_t *)a.ws;
-    int32_t *order = (int32_t *)((char *)a.ws + align256((size_t)N * 4));
-    hipLaunchKernelGGL(rank_kernel, dim3((unsigned)ceil_div(N, 256)), dim3(256), 0, s, a.tokens, N, a.V, key, order);
+    const GradWs w = layout(a.ws, N, a.I, a.V);
+    const Sorted q = {w.rank, w.key, w.start};
+    const int R = std::min(SORT_MOST, (int)ceil_div(a.V, 256));
+    hipLaunchKernelGGL(sort_kernel, dim3((unsigned)ceil_div(a.V, R)), dim3(SORT_NT), 0, s, a.tokens, N, a.V, R, w.rank,
+                       w.key, w.start);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(embed_grad_kernel, dim3((unsigned)a.V), dim3(256), 0, s, a, N, key, order);
-    return hipGetLastError();
+    const Tiling g = tiling_of(a.T, a.B, a.I);
+    const long tiles = (long)g.T * g.chunks * g.tiles;
+    const long zeros = a.accumulate ? 0 : ceil_div(a.V, ZERO_ROWS);
+    const bool aligned = a.I % 4 == 0 && (uintptr_t)a.dE % 16 == 0;
+    hipLaunchKernelGGL(turn_kernel, dim3((unsigned)(tiles + zeros)), dim3(NT), 0, s, a, g, q, w.rows, tiles,
+                       (uintptr_t)a.dX % 16 == 0, aligned);
+    if ((e = hipGetLastError()) != hipSuccess)
+        return e;
+    return group_of(N) == 16 ? walk<16>(a, q, w, N, aligned, s) : walk<64>(a, q, w, N, aligned, s);
 }
 
 } // namespace lstmss

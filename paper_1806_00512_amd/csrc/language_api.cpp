@@ -41,12 +41,13 @@ int32_t check_tokens(const lstmss_tokens *d, bool dtype) {
                     d->B, d->I, d->V);
     if (dtype && d->dtype != LSTMSS_F32 && d->dtype != LSTMSS_BF16)
         return fail(LSTMSS_ERR_UNSUPPORTED, "unknown dtype %d", d->dtype);
-    // grids of a work-group for 64 tokens, or for a step, stay below 2^32 threads;
-    // indices within a step, a row number and one past it fit 32 bits
-    const int64_t N = (int64_t)d->T * d->B, m31 = (int64_t)1 << 31, m40 = (int64_t)1 << 40;
-    const int64_t w = d->V > d->I ? d->V : d->I, r = d->B > d->I ? d->B : d->I;
-    if (d->T > 1 << 22 || N >= (int64_t)1 << 29 || (int64_t)d->V * r >= m31 || d->V >= m31 - 65536 ||
-        (int64_t)d->I * d->B >= m31 || N * w >= m40)
+    // indices within a step and row numbers fit 32 bits; grids (a work-group for
+    // each step and 40 or more of its columns, and for 64 features of these, or
+    // for 16 rows of the table) stay below 2^32 threads
+    const int64_t N = (int64_t)d->T * d->B, m31 = (int64_t)1 << 31;
+    const int64_t steps = (int64_t)d->T * (d->B / 33 + 1), tiles = steps * (d->I / 64 + 1);
+    if (N >= (int64_t)1 << 28 || d->V > 1 << 26 || (int64_t)d->V * d->B >= m31 || (int64_t)d->V * d->I >= m31 ||
+        (int64_t)d->I * d->B >= m31 || tiles >= (int64_t)1 << 23)
         return fail(LSTMSS_ERR_UNSUPPORTED, "sizes too large");
     return LSTMSS_OK;
 }

@@ -26,27 +26,31 @@ __device__ __forceinline__ void philox(uint64_t counter, uint32_t k0, uint32_t k
     out[3] = c3;
 }
 
-// The 16 bits number k of a counter's 128.
-__device__ __forceinline__ uint32_t drop_bits(const uint32_t w[4], int k) {
-    return k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xffffu;
-}
-
-// The element a mask index e of a drop with a period stands at.
-__device__ __forceinline__ long drop_index(const DropArgs &d, long e) {
-    return d.period > 0 ? e % d.period : e;
-}
-
-// Element e of a tensor, with dropout: +0 where dropped, whatever v is.
-__device__ __forceinline__ float drop_one(const DropArgs &d, long e, float v) {
+// Dropout of the eight elements e .. e + 7 (e a multiple of 8): +0 where
+// dropped, whatever f holds.  One counter gives all eight, unless the mask
+// repeats after a length that is no multiple of 8.
+__device__ __forceinline__ void drop8(const DropArgs &d, long e, float *f) {
     if (d.thr == 0)
-        return v;
-    const long m = drop_index(d, e);
+        return;
     uint32_t w[4];
-    philox(d.counter + (uint64_t)(m >> 3), d.key0, d.key1, w);
-    const int k = (int)(m & 7);
-    const uint32_t word = k < 4 ? (k < 2 ? w[0] : w[1]) : (k < 6 ? w[2] : w[3]);
-    const uint32_t bits = k & 1 ? word >> 16 : word & 0xffffu;
-    return bits >= d.thr ? v * d.scale : 0.f;
+    if ((d.period & 7) == 0) {
+        const long m = d.period > 0 ? e % d.period : e;
+        philox(d.counter + (uint64_t)(m >> 3), d.key0, d.key1, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t bits = k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xffffu;
+            f[k] = bits >= d.thr ? f[k] * d.scale : 0.f;
+        }
+        return;
+    }
+    for (int k = 0; k < 8; ++k) {
+        const long m = (e + k) % d.period;
+        philox(d.counter + (uint64_t)(m >> 3), d.key0, d.key1, w);
+        const int h = (int)(m & 7);
+        const uint32_t word = h < 4 ? (h < 2 ? w[0] : w[1]) : (h < 6 ? w[2] : w[3]);
+        const uint32_t bits = h & 1 ? word >> 16 : word & 0xffffu;
+        f[k] = bits >= d.thr ? f[k] * d.scale : 0.f;
+    }
 }
 
 } // namespace lstmss

@@ -59,4 +59,16 @@ struct vec<bf16_t, 8> {
     }
 };
 
+// Eight elements from a 16-byte boundary.
+__device__ __forceinline__ void load8(const float *p, float *f) {
+    vec<float, 4>::load(p, f);
+    vec<float, 4>::load(p + 4, f + 4);
+}
+__device__ __forceinline__ void load8(const bf16_t *p, float *f) { vec<bf16_t, 8>::load(p, f); }
+__device__ __forceinline__ void store8(float *p, const float *f) {
+    vec<float, 4>::store(p, f);
+    vec<float, 4>::store(p + 4, f + 4);
+}
+__device__ __forceinline__ void store8(bf16_t *p, const float *f) { vec<bf16_t, 8>::store(p, f); }
+
 } // namespace lstmss
