@@ -7,11 +7,10 @@
 //
 // Gradient: dE[v][i] = scale * sum of dX[t][i][b] over the (t, b) with token v.
 //   sort_kernel   the positions' ranks by (token, position), and each token's
-//                 range of ranks
+//                 range of ranks; dE is zeroed by the same launch
 //   turn_kernel   dX turned over as in the lookup, each position's row written
-//                 at its rank (the row of a token that stands once goes straight
-//                 into dE); rows of tokens that do not occur are zeroed by the
-//                 same launch
+//                 at its rank (the row of a token that stands once goes
+//                 straight into dE)
 //   walk_kernel   sums of equal tokens' rows, which now follow one another, over
 //                 groups of rows
 //   carry_kernel  tokens whose rows lie in several groups
@@ -54,11 +53,12 @@ __device__ __forceinline__ Tile tile_of(const Tiling &g, long block) {
     return a;
 }
 
-// Calls f(e, lo, hi, i, b) for the groups of eight elements e .. e + 7 (e a
+// Calls f(e, lo, hi, i, b, whole) for the groups of eight elements e .. e + 7 (e a
 // multiple of 8) that cover a tile of the batch-last tensor, those in [lo, hi)
 // its own: element e + k is of column b + k, feature i while b + k < B, of the
 // next features from there.  b may be negative down to -7 in a group that
-// begins before its piece.
+// begins before its piece.  `whole` holds for a group that is its tile's alone
+// and of one feature, which all are where B is a multiple of 8.
 template <class F>
 __device__ __forceinline__ void for_groups(const Tiling &g, const Tile &a, F &&f) {
     if (g.chunks == 1) {
@@ -66,8 +66,8 @@ __device__ __forceinline__ void for_groups(const Tiling &g, const Tile &a, F &&f
         const long q0 = lo >> 3, q1 = (hi + 7) >> 3;
         for (long q = q0 + threadIdx.x; q < q1; q += NT) {
             const int r = (int)(q * 8 - lo);
-            const int i = r < 0 ? 0 : r / g.B;
-            f(q * 8, lo, hi, i, r - i * g.B);
+            const int i = r < 0 ? 0 : r / g.B, b = r - i * g.B;
+            f(q * 8, lo, hi, i, b, r >= 0 && q * 8 + 8 <= hi && b + 8 <= g.B);
         }
     } else {
         const int per = (a.nb + 7) / 8 + 1;
@@ -76,7 +76,7 @@ __device__ __forceinline__ void for_groups(const Tiling &g, const Tile &a, F &&f
             const long lo = ((long)a.t * g.I + a.i0 + i) * g.B + a.b0, hi = lo + a.nb;
             const long e = (lo >> 3) * 8 + j * 8;
             if (e < hi)
-                f(e, lo, hi, i, (int)(e - lo));
+                f(e, lo, hi, i, (int)(e - lo), e >= lo && e + 8 <= hi);
         }
     }
 }
@@ -104,8 +104,15 @@ __global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, bool a
     }
     __syncthreads();
     TS *x = (TS *)a.x;
-    for_groups(g, w, [&](long e, long lo, long hi, int i, int b) {
+    for_groups(g, w, [&](long e, long lo, long hi, int i, int b, bool whole) {
         float f[8];
+        if (whole && aligned) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                f[k] = tile[(b + k) * PITCH + i] * a.scale;
+            drop8(a.drop, e, f);
+            return store8(x + e, f);
+        }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const bool in = e + k >= lo && e + k < hi;
@@ -116,8 +123,6 @@ __global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, bool a
             }
         }
         drop8(a.drop, e, f);
-        if (aligned && e >= lo && e + 8 <= hi)
-            return store8(x + e, f);
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             if (e + k >= lo && e + k < hi)
@@ -129,13 +134,32 @@ __global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, bool a
 
 constexpr int SORT_NT = 1024, SORT_WAVES = SORT_NT / 64, SORT_MOST = 512;
 
+constexpr long FILL = 65536; // elements that a work-group zeroes
+
+__device__ __forceinline__ void zero_fill(float *p, long i0, long i1) {
+    // whole vectors between the first and the last 16-byte boundary, the rest singly
+    const long v0 = i0 + (4 - (long)((uintptr_t)(p + i0) / 4 % 4)) % 4, v1 = i1 - (long)((uintptr_t)(p + i1) / 4 % 4);
+    for (long i = v0 + threadIdx.x * 4; i < v1; i += SORT_NT * 4)
+        *(f32x4 *)(p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
+    if ((long)threadIdx.x < v0 - i0 && i0 + (long)threadIdx.x < i1)
+        p[i0 + threadIdx.x] = 0.f;
+    if (v1 >= v0 && (long)threadIdx.x < i1 - v1)
+        p[v1 + threadIdx.x] = 0.f;
+}
+
 // Work-group w places the tokens [w R, (w + 1) R): every wave counts its share
 // of the positions by token; the counts before a (wave, token), with those of
 // all smaller tokens, are where that wave's first position of the token goes,
 // and the waves then go over their shares again in order.  Every work-group
 // reads all tokens, which lie in the caches; none waits for another.
+// The work-groups from `sorters` on zero dE meanwhile, which the sort leaves
+// the memory free for: rows in use are written after this launch.
 __global__ __launch_bounds__(SORT_NT) void sort_kernel(const int32_t *tokens, int N, int V, int R, int32_t *rank,
-                                                       int32_t *key, int32_t *start) {
+                                                       int32_t *key, int32_t *start, int sorters, float *dE, long size) {
+    if ((int)blockIdx.x >= sorters) {
+        const long i0 = (long)(blockIdx.x - sorters) * FILL, i1 = min(size, i0 + FILL);
+        return zero_fill(dE, i0, i1);
+    }
     __shared__ int hist[SORT_WAVES][SORT_MOST];
     __shared__ int less[SORT_WAVES], sums[SORT_WAVES];
     const int lo = blockIdx.x * R, n = min(V - lo, R);
@@ -187,24 +211,26 @@ __global__ __launch_bounds__(SORT_NT) void sort_kernel(const int32_t *tokens, in
         }
     }
     __syncthreads();
+    // 64 positions at once: the lanes with a lane's token are those that agree
+    // with it in every bit of the token's place in the range
     volatile int *next = hist[w];
+    const int bits = 32 - __clz(R - 1);
+    const uint64_t below = (1ull << lane) - 1;
     for (int base = p0; base < p1; base += 64) {
         const int p = base + lane;
-        const int v = p < p1 ? tokens[p] : -1;
-        const bool in = (uint32_t)v - (uint32_t)lo < (uint32_t)n;
-        for (uint64_t left = __ballot(in); left;) {
-            const int l = __ffsll((long long)left) - 1;
-            const int token = __shfl(v, l, 64);
-            const uint64_t same = __ballot(in && v == token);
-            const int first = next[token - lo];
-            if (in && v == token) {
-                const int r = first + __popcll(same & ((1ull << lane) - 1));
-                rank[p] = r;
-                key[r] = v;
-            }
-            if (lane == l)
-                next[token - lo] = first + __popcll(same);
-            left &= ~same;
+        const uint32_t k = (uint32_t)(p < p1 ? tokens[p] : -1) - (uint32_t)lo;
+        const bool in = k < (uint32_t)n;
+        uint64_t same = __ballot(in);
+        for (int j = 0; j < bits; ++j) {
+            const uint64_t one = __ballot(k >> j & 1);
+            same &= k >> j & 1 ? one : ~one;
+        }
+        if (in) {
+            const int first = next[k], r = first + __popcll(same & below);
+            rank[p] = r;
+            key[r] = lo + (int)k;
+            if ((same & below) == 0)
+                next[k] = first + __popcll(same);
         }
     }
 }
@@ -218,31 +244,10 @@ __device__ __forceinline__ void put(const EmbedGradArgs &a, float *p, float sum)
     *p = a.accumulate ? *p + sum * a.scale : sum * a.scale;
 }
 
-constexpr int ZERO_ROWS = 16; // rows of dE that a work-group looks at
-
-__device__ __forceinline__ void zero_rows(const EmbedGradArgs &a, const int32_t *start, long block, bool aligned) {
-    const int v0 = (int)(block * ZERO_ROWS), v1 = (int)min((long)a.V, (block + 1) * ZERO_ROWS);
-    for (int v = v0; v < v1; ++v) {
-        if (start[v] != start[v + 1])
-            continue;
-        float *p = a.dE + (long)v * a.I;
-        if (aligned) {
-            for (int i = threadIdx.x * 4; i < a.I; i += NT * 4)
-                *(f32x4 *)(p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
-        } else {
-            for (int i = threadIdx.x; i < a.I; i += NT)
-                p[i] = 0.f;
-        }
-    }
-}
-
-__global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sorted q, float *rows, long tiles,
-                                                  bool aligned, bool zero_aligned) {
+__global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sorted q, float *rows, bool aligned) {
     __shared__ float tile[TILE * PITCH];
     __shared__ float *dest[TILE];
     __shared__ bool once[TILE];
-    if (blockIdx.x >= tiles)
-        return zero_rows(a, q.start, blockIdx.x - tiles, zero_aligned);
     const Tile w = tile_of(g, blockIdx.x);
     if ((int)threadIdx.x < w.nb) {
         const long p = (long)w.t * g.B + w.b0 + threadIdx.x;
@@ -256,8 +261,16 @@ __global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sor
         dest[threadIdx.x] = d;
         once[threadIdx.x] = one;
     }
-    for_groups(g, w, [&](long e, long lo, long hi, int i, int b) {
+    for_groups(g, w, [&](long e, long lo, long hi, int i, int b, bool whole) {
         float f[8];
+        if (whole && aligned) {
+            load8(a.dX + e, f);
+            drop8(a.drop, e, f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                tile[(b + k) * PITCH + i] = f[k];
+            return;
+        }
         if (aligned && e >= lo && e + 8 <= hi) {
             load8(a.dX + e, f);
         } else {
@@ -398,7 +411,7 @@ Tiling tiling_of(int T, int B, int I) {
 }
 
 // Rows of a group of the walk: more groups while there are few rows.
-int group_of(int N) { return N < 4096 ? 16 : 64; }
+int group_of(int N) { return N < 32768 ? 16 : 64; }
 
 struct GradWs {
     int32_t *rank, *key, *start;
@@ -467,17 +480,17 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
     const GradWs w = layout(a.ws, N, a.I, a.V);
     const Sorted q = {w.rank, w.key, w.start};
     const int R = std::min(SORT_MOST, (int)ceil_div(a.V, 256));
-    hipLaunchKernelGGL(sort_kernel, dim3((unsigned)ceil_div(a.V, R)), dim3(SORT_NT), 0, s, a.tokens, N, a.V, R, w.rank,
-                       w.key, w.start);
+    const long size = (long)a.V * a.I, sorters = ceil_div(a.V, R), fills = a.accumulate ? 0 : ceil_div(size, FILL);
+    hipLaunchKernelGGL(sort_kernel, dim3((unsigned)(sorters + fills)), dim3(SORT_NT), 0, s, a.tokens, N, a.V, R, w.rank,
+                       w.key, w.start, (int)sorters, a.dE, size);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
     const Tiling g = tiling_of(a.T, a.B, a.I);
     const long tiles = (long)g.T * g.chunks * g.tiles;
-    const long zeros = a.accumulate ? 0 : ceil_div(a.V, ZERO_ROWS);
     const bool aligned = a.I % 4 == 0 && (uintptr_t)a.dE % 16 == 0;
-    hipLaunchKernelGGL(turn_kernel, dim3((unsigned)(tiles + zeros)), dim3(NT), 0, s, a, g, q, w.rows, tiles,
-                       (uintptr_t)a.dX % 16 == 0, aligned);
+    hipLaunchKernelGGL(turn_kernel, dim3((unsigned)tiles), dim3(NT), 0, s, a, g, q, w.rows,
+                       (uintptr_t)a.dX % 16 == 0);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
     return group_of(N) == 16 ? walk<16>(a, q, w, N, aligned, s) : walk<64>(a, q, w, N, aligned, s);

@@ -595,38 +595,49 @@ def _drop_ptr(d):
     return ctypes.byref(d)
 
 
+# The current stream of a GPU as a plain number; torch.cuda.current_stream()
+# builds an object around it, which takes as long as half a kernel launch.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _on(first, name, stream):
-    """The stream of a call whose tensors live where `first` does, as (torch stream, pointer)."""
+    """(index of the GPU that `first` lives on, the call's stream there)."""
     if not isinstance(first, torch.Tensor):
         raise TypeError("%s must be a torch tensor" % name)
-    if first.device.type != "cuda":
+    if not first.is_cuda:
         raise ValueError("%s must live on the GPU" % name)
-    if first.device.index != torch.cuda.current_device():
-        raise ValueError("%s lives on %s, which is not the current GPU" % (name, first.device))
-    s = stream if stream is not None else torch.cuda.current_stream()
-    if s.device != first.device:
-        raise ValueError("the stream is of %s, %s lives on %s" % (s.device, name, first.device))
-    return s, ctypes.c_void_p(s.cuda_stream)
+    dev = first.get_device()
+    if dev != torch.cuda.current_device():
+        raise ValueError("%s lives on cuda:%d, which is not the current GPU" % (name, dev))
+    if stream is None:
+        return dev, _raw_stream(dev) if _raw_stream else torch.cuda.current_stream().cuda_stream
+    if stream.device.index != dev:
+        raise ValueError("the stream is of %s, %s lives on cuda:%d" % (stream.device, name, dev))
+    return dev, stream.cuda_stream
+
+
+def _at(t, dtype, shape, dev, name):
+    """Address of a tensor that is what it has to be (shape None: any), else the error."""
+    if t is None:
+        return None
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev
+            and (shape is None or t.shape == shape) and t.is_contiguous()):
+        return t.data_ptr()
+    _ptr(t, dtype, shape, name)
+    raise ValueError("%s lives on %s, expected cuda:%d" % (name, t.device, dev))
 
 
 def _sizes(T, B, I, V, dtype) -> Tokens:
-    n = [int(k) for k in (T, B, I, V)]
-    if max(n) >= 2**31 or min(n) < -2**31:
-        raise ValueError("sizes %s must fit 32 bits" % n)
-    return Tokens(*n, _dt(dtype))
+    if max(T, B, I, V) >= 2**31 or min(T, B, I, V) < -2**31:
+        raise ValueError("sizes %s must fit 32 bits" % ((T, B, I, V),))
+    return Tokens(T, B, I, V, _dt(dtype))
 
 
-def _near(dev, **tensors):
-    for name, t in tensors.items():
-        if isinstance(t, torch.Tensor) and t.device != dev:
-            raise ValueError("%s lives on %s, expected %s" % (name, t.device, dev))
-
-
-def _new(shape, dtype, dev, s, stream):
-    """A tensor that work on stream s will use (s may not be the one it is allocated for)."""
+def _new(shape, dtype, dev, stream):
+    """A tensor that work on `stream` (None: the current one, for which it is allocated) will use."""
     t = torch.empty(shape, dtype=dtype, device=dev)
     if stream is not None:
-        t.record_stream(s)
+        t.record_stream(stream)
     return t
 
 
@@ -638,15 +649,14 @@ def _bytes(n, what):
 def dropout(x, drop, out=None, stream=None):
     """x with dropout (see drop()), any shape; out may be x.  The gradient of x
     is dropout(gradient of out, the same drop)."""
-    s, sp = _on(x, "x", stream)
+    dev, sp = _on(x, "x", stream)
     dt = _dt(x.dtype)
     if drop is None:
         raise TypeError("drop must be made by drop()")
     if out is None:
-        out = _new(x.shape, x.dtype, x.device, s, stream)
-    _near(x.device, out=out)
-    rc = load().lstmss_dropout(x.numel(), dt, _drop_ptr(drop), _ptr(x, name="x"),
-                               _ptr(out, x.dtype, x.shape, "out"), sp)
+        out = _new(x.shape, x.dtype, x.device, stream)
+    rc = load().lstmss_dropout(x.numel(), dt, _drop_ptr(drop), _at(x, x.dtype, None, dev, "x"),
+                               _at(out, x.dtype, x.shape, dev, "out"), sp)
     _check(rc, "lstmss_dropout")
     return out
 
@@ -654,17 +664,16 @@ def dropout(x, drop, out=None, stream=None):
 def embed(tokens, E, scale=1.0, drop=None, out=None, stream=None):
     """x [T][I][B] = scale * E[tokens] of tokens [T][B] (int32; outside [0, V): zeros)
     and a table E [V][I] (fp32 or bf16), with dropout over x where drop is given."""
-    s, sp = _on(tokens, "tokens", stream)
-    _near(tokens.device, E=E, out=out)
+    dev, sp = _on(tokens, "tokens", stream)
     if tokens.dim() != 2 or E.dim() != 2:
         raise ValueError("tokens must be [T][B] and E [V][I]")
-    (T, B), (V, I) = tokens.shape, E.shape
-    d = _sizes(T, B, I, V, E.dtype)
+    (T, B), (V, I), dt = tokens.shape, E.shape, E.dtype
+    d = _sizes(T, B, I, V, dt)
     if out is None:
-        out = _new((T, I, B), E.dtype, E.device, s, stream)
-    rc = load().lstmss_embed(ctypes.byref(d), _ptr(E, name="E"),
-                             _ptr(tokens, torch.int32, name="tokens"), float(scale),
-                             _drop_ptr(drop), _ptr(out, E.dtype, (T, I, B), "out"), sp)
+        out = _new((T, I, B), dt, tokens.device, stream)
+    rc = load().lstmss_embed(ctypes.byref(d), _at(E, dt, None, dev, "E"),
+                             _at(tokens, torch.int32, None, dev, "tokens"), float(scale),
+                             _drop_ptr(drop), _at(out, dt, (T, I, B), dev, "out"), sp)
     _check(rc, "lstmss_embed")
     return out
 
@@ -679,23 +688,21 @@ def embed_grad(tokens, dX, V, scale=1.0, drop=None, accumulate=False, dE=None, w
                stream=None):
     """Gradient of embed: dE [V][I] fp32 from dX [T][I][B] fp32, overwritten or
     (accumulate, with dE given) added to."""
-    s, sp = _on(tokens, "tokens", stream)
-    _near(tokens.device, dX=dX, dE=dE, ws=ws)
+    dev, sp = _on(tokens, "tokens", stream)
     if tokens.dim() != 2 or dX.dim() != 3:
         raise ValueError("tokens must be [T][B] and dX [T][I][B]")
-    (T, B), I, V = tokens.shape, dX.shape[1], int(V)
+    (T, B), I, V, f32 = tokens.shape, dX.shape[1], int(V), torch.float32
     d = _sizes(T, B, I, V, F32)
     if dE is None:
         if accumulate:
             raise ValueError("accumulate needs dE")
-        dE = _new((V, I), torch.float32, dX.device, s, stream)
+        dE = _new((d.V, I), f32, tokens.device, stream)
     if ws is None:
-        ws = _new(embed_grad_workspace_bytes(T, B, I, V), torch.uint8, dX.device, s, stream)
-    rc = load().lstmss_embed_grad(ctypes.byref(d), _ptr(tokens, torch.int32, name="tokens"),
-                                  _ptr(dX, torch.float32, (T, I, B), "dX"), float(scale),
-                                  _drop_ptr(drop), 1 if accumulate else 0,
-                                  _ptr(dE, torch.float32, (V, I), "dE"),
-                                  _ptr(ws, torch.uint8, name="ws"), ws.numel(), sp)
+        ws = _new(embed_grad_workspace_bytes(T, B, I, V), torch.uint8, tokens.device, stream)
+    rc = load().lstmss_embed_grad(ctypes.byref(d), _at(tokens, torch.int32, None, dev, "tokens"),
+                                  _at(dX, f32, (T, I, B), dev, "dX"), float(scale), _drop_ptr(drop),
+                                  1 if accumulate else 0, _at(dE, f32, (d.V, I), dev, "dE"),
+                                  _at(ws, torch.uint8, None, dev, "ws"), ws.numel(), sp)
     _check(rc, "lstmss_embed_grad")
     return dE
 
@@ -707,46 +714,45 @@ def loss_workspace_bytes(T, B, V, dtype=F32) -> int:
                   "lstmss_loss_workspace_bytes")
 
 
-def _loss_args(logits, targets, ws, stream, **tokens):
-    """What the three loss calls share: sizes, workspace, stream, pointers."""
-    s, sp = _on(logits, "logits", stream)
-    _near(logits.device, targets=targets, ws=ws, **tokens)
+def _loss_args(logits, targets, ws, stream):
+    """What the three loss calls share: GPU, stream, sizes, workspace and the addresses of
+    the logits, the targets and the workspace."""
+    dev, sp = _on(logits, "logits", stream)
     if logits.dim() != 3:
         raise ValueError("logits must be [T][V][B]")
     T, V, B = logits.shape
-    d = _sizes(T, B, 1, V, logits.dtype)
+    dt = logits.dtype
+    d = _sizes(T, B, 1, V, dt)
     if ws is None:
-        ws = _new(loss_workspace_bytes(T, B, V, logits.dtype), torch.uint8, logits.device, s,
-                  stream)
-    f32 = torch.float32
-    return (d, s, sp, ws, _ptr(logits, name="logits"),
-            _ptr(targets, torch.int32, (T, B), "targets"),
-            {k: _ptr(t, f32, (T, B), k) for k, t in tokens.items()})
+        ws = _new(loss_workspace_bytes(T, B, V, dt), torch.uint8, logits.device, stream)
+    return (dev, sp, d, ws, _at(logits, dt, None, dev, "logits"),
+            _at(targets, torch.int32, (T, B), dev, "targets"),
+            _at(ws, torch.uint8, None, dev, "ws"))
 
 
-def _loss_out(logits, out, want_grad, s, stream):
-    T, V, B = logits.shape
-    o, dev = dict(out or {}), logits.device
-    for k, shape, dt in (("loss", (1,), torch.float32), ("logp", (T, B), torch.float32),
-                         ("dlogits", (T, V, B), logits.dtype)):
-        if o.get(k) is None and (want_grad or k != "dlogits"):
-            o[k] = _new(shape, dt, dev, s, stream)
-    _near(dev, **o)
-    return o, (_ptr(o["loss"], torch.float32, (1,), "loss"),
-               _ptr(o["logp"], torch.float32, (T, B), "logp"),
-               _ptr(o["dlogits"], logits.dtype, (T, V, B), "dlogits") if want_grad else None)
+def _loss_out(logits, out, want_grad, dev, d, stream):
+    """The dict of outputs (given or new) and the addresses of loss, logp and dlogits."""
+    o, f32, each = dict(out) if out else {}, torch.float32, (d.T, d.B)
+    if o.get("loss") is None:
+        o["loss"] = _new((1,), f32, logits.device, stream)
+    if o.get("logp") is None:
+        o["logp"] = _new(each, f32, logits.device, stream)
+    if want_grad and o.get("dlogits") is None:
+        o["dlogits"] = _new(logits.shape, logits.dtype, logits.device, stream)
+    return o, (_at(o["loss"], f32, (1,), dev, "loss"), _at(o["logp"], f32, each, dev, "logp"),
+               _at(o["dlogits"], logits.dtype, logits.shape, dev, "dlogits") if want_grad
+               else None)
 
 
 def token_logp(logits, targets, logp=None, ws=None, stream=None):
     """logp [T][B] fp32: log softmax over the middle axis of logits [T][V][B] (fp32
     or bf16) at targets [T][B] (int32; outside [0, V): 0)."""
-    d, s, sp, ws, px, py, _ = _loss_args(logits, targets, ws, stream)
+    dev, sp, d, ws, px, py, pw = _loss_args(logits, targets, ws, stream)
     if logp is None:
-        logp = _new((d.T, d.B), torch.float32, logits.device, s, stream)
-    _near(logits.device, logp=logp)
+        logp = _new((d.T, d.B), torch.float32, logits.device, stream)
     rc = load().lstmss_token_logp(ctypes.byref(d), px, py,
-                                  _ptr(logp, torch.float32, (d.T, d.B), "logp"),
-                                  _ptr(ws, torch.uint8, name="ws"), ws.numel(), sp)
+                                  _at(logp, torch.float32, (d.T, d.B), dev, "logp"), pw,
+                                  ws.numel(), sp)
     _check(rc, "lstmss_token_logp")
     return logp
 
@@ -756,11 +762,12 @@ def xent(logits, targets, weights=None, scale=None, want_grad=True, out=None, ws
     """Cross entropy -scale * sum of weights * logp (scale: 1 / B unless given).
     Returns dict(loss [1], logp [T][B], dlogits like logits); out: tensors to
     write those to (dlogits may be logits itself)."""
-    d, s, sp, ws, px, py, p = _loss_args(logits, targets, ws, stream, weights=weights)
-    o, (pl, pp, pg) = _loss_out(logits, out, want_grad, s, stream)
-    rc = load().lstmss_xent(ctypes.byref(d), px, py, p["weights"],
-                            1.0 / d.B if scale is None else float(scale), pl, pp, pg,
-                            _ptr(ws, torch.uint8, name="ws"), ws.numel(), sp)
+    dev, sp, d, ws, px, py, pw = _loss_args(logits, targets, ws, stream)
+    o, (pl, pp, pg) = _loss_out(logits, out, want_grad, dev, d, stream)
+    rc = load().lstmss_xent(ctypes.byref(d), px, py,
+                            _at(weights, torch.float32, (d.T, d.B), dev, "weights"),
+                            1.0 / d.B if scale is None else float(scale), pl, pp, pg, pw,
+                            ws.numel(), sp)
     _check(rc, "lstmss_xent")
     return o
 
@@ -770,14 +777,16 @@ def policy_loss(logits, targets, old, ref, adv, weights=None, clip_low=0.2, clip
     """Clipped policy loss with a KL term (see lstmss_policy_loss): old, ref (None:
     the logits' own logp; no KL term), adv and weights are [T][B] fp32.  Returns
     and takes the outputs of xent."""
-    d, s, sp, ws, px, py, p = _loss_args(logits, targets, ws, stream, old=old, ref=ref, adv=adv,
-                                         weights=weights)
-    o, (pl, pp, pg) = _loss_out(logits, out, want_grad, s, stream)
+    dev, sp, d, ws, px, py, pw = _loss_args(logits, targets, ws, stream)
+    o, (pl, pp, pg) = _loss_out(logits, out, want_grad, dev, d, stream)
+    f32, each = torch.float32, (d.T, d.B)
     q = Policy(float(clip_low), float(clip_high), float(kl),
                1.0 / d.B if scale is None else float(scale))
-    rc = load().lstmss_policy_loss(ctypes.byref(d), ctypes.byref(q), px, py, p["old"], p["ref"],
-                                   p["adv"], p["weights"], pl, pp, pg,
-                                   _ptr(ws, torch.uint8, name="ws"), ws.numel(), sp)
+    rc = load().lstmss_policy_loss(ctypes.byref(d), ctypes.byref(q), px, py,
+                                   _at(old, f32, each, dev, "old"), _at(ref, f32, each, dev, "ref"),
+                                   _at(adv, f32, each, dev, "adv"),
+                                   _at(weights, f32, each, dev, "weights"), pl, pp, pg, pw,
+                                   ws.numel(), sp)
     _check(rc, "lstmss_policy_loss")
     return o
 
