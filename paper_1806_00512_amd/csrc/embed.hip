@@ -81,29 +81,10 @@ __device__ __forceinline__ void for_groups(const Tiling &g, const Tile &a, F &&f
     }
 }
 
-template <typename TS, int LV>
-__global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, bool aligned) {
-    __shared__ float tile[TILE * PITCH];
-    __shared__ int row[TILE];
-    const Tile w = tile_of(g, blockIdx.x);
-    if ((int)threadIdx.x < w.nb) {
-        const int v = a.tokens[(long)w.t * g.B + w.b0 + threadIdx.x];
-        row[threadIdx.x] = (uint32_t)v < (uint32_t)a.V ? v : -1;
-    }
-    __syncthreads();
-    constexpr int PER = TILE / LV;
-    const TS *E = (const TS *)a.E;
-    for (int n = threadIdx.x; n < w.nb * PER; n += NT) {
-        const int b = n / PER, i = (n - b * PER) * LV;
-        float f[LV] = {};
-        if (row[b] >= 0 && i < w.ni)
-            vec<TS, LV>::load(E + (long)row[b] * g.I + w.i0 + i, f);
-#pragma unroll
-        for (int k = 0; k < LV; ++k)
-            tile[b * PITCH + i + k] = f[k];
-    }
-    __syncthreads();
-    TS *x = (TS *)a.x;
+// A tile's elements, scaled and with dropout, from LDS to x.
+template <typename TS>
+__device__ __forceinline__ void write_tile(const EmbedArgs &a, const Tiling &g, const Tile &w, const float *tile, TS *x,
+                                           bool aligned) {
     for_groups(g, w, [&](long e, long lo, long hi, int i, int b, bool whole) {
         float f[8];
         if (whole && aligned) {
@@ -128,6 +109,58 @@ __global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, bool a
             if (e + k >= lo && e + k < hi)
                 st<TS>::store(x, e + k, f[k]);
     });
+}
+
+// A work-group's columns and `run` feature tiles one after the other: the next
+// tile's rows are on their way while this one is turned over and written.
+template <typename TS, int LV>
+__global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int run, bool aligned) {
+    constexpr int PER = TILE / LV, LOADS = TILE * PER / NT;
+    __shared__ float tile[TILE * PITCH];
+    const int runs = (g.tiles + run - 1) / run;
+    const int part = blockIdx.x % runs;
+    const long steps = blockIdx.x / runs;
+    const int last = min(g.tiles, (part + 1) * run);
+    Tile w = tile_of(g, steps * g.tiles + part * run);
+    const TS *row[LOADS];
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) {
+        const int b = (threadIdx.x + k * NT) / PER;
+        const int v = b < w.nb ? a.tokens[(long)w.t * g.B + w.b0 + b] : -1;
+        row[k] = (uint32_t)v < (uint32_t)a.V ? (const TS *)a.E + (long)v * g.I : nullptr;
+    }
+    float f[LOADS][LV];
+    const int i = threadIdx.x % PER * LV;
+    auto fetch = [&](int i0) {
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            if (row[k] && i0 + i < g.I) {
+                vec<TS, LV>::load(row[k] + i0 + i, f[k]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < LV; ++j)
+                    f[k][j] = 0.f;
+            }
+        }
+    };
+    fetch(w.i0);
+    TS *x = (TS *)a.x;
+    for (int n = part * run; n < last; ++n) {
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            const int b = (threadIdx.x + k * NT) / PER;
+#pragma unroll
+            for (int j = 0; j < LV; ++j)
+                tile[b * PITCH + i + j] = f[k][j];
+        }
+        __syncthreads();
+        w.i0 = n * TILE;
+        w.ni = min(TILE, g.I - w.i0);
+        if (n + 1 < last)
+            fetch(w.i0 + TILE);
+        write_tile(a, g, w, tile, x, aligned);
+        __syncthreads();
+    }
 }
 
 // ------------------------------------------------------------ gradient
@@ -441,12 +474,15 @@ template <typename TS>
 hipError_t lookup(const EmbedArgs &a, hipStream_t s) {
     constexpr int LV = vec_of<TS>();
     const Tiling g = tiling_of(a.T, a.B, a.I);
-    const dim3 grid((unsigned)((long)g.T * g.chunks * g.tiles));
+    // runs of up to four tiles while 2048 work-groups (eight on a CU) are left
+    const long steps = (long)g.T * g.chunks;
+    const int run = (int)std::max(1L, std::min(4L, steps * g.tiles / 2048));
+    const dim3 grid((unsigned)(steps * ceil_div(g.tiles, run)));
     const bool aligned = (uintptr_t)a.x % 16 == 0;
     if ((uintptr_t)a.E % 16 == 0 && a.I % LV == 0)
-        hipLaunchKernelGGL((embed_kernel<TS, LV>), grid, dim3(NT), 0, s, a, g, aligned);
+        hipLaunchKernelGGL((embed_kernel<TS, LV>), grid, dim3(NT), 0, s, a, g, run, aligned);
     else
-        hipLaunchKernelGGL((embed_kernel<TS, 1>), grid, dim3(NT), 0, s, a, g, aligned);
+        hipLaunchKernelGGL((embed_kernel<TS, 1>), grid, dim3(NT), 0, s, a, g, run, aligned);
     return hipGetLastError();
 }
 
