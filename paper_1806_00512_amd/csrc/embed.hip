@@ -81,6 +81,20 @@ __device__ __forceinline__ void for_groups(const Tiling &g, const Tile &a, F &&f
     }
 }
 
+// Calls f(e, i, b) for the groups of a tile of 64 whole columns: eight to a
+// feature, each of that feature alone.
+template <class F>
+__device__ __forceinline__ void for_whole_groups(const Tiling &g, const Tile &a, F &&f) {
+    const long lo = ((long)a.t * g.I + a.i0) * g.B + a.b0;
+    const int b = (threadIdx.x & 7) * 8;
+#pragma unroll
+    for (int n = 0; n < TILE * 8 / NT; ++n) {
+        const int i = (threadIdx.x >> 3) + n * (NT / 8);
+        if (i < a.ni)
+            f(lo + i * g.B + b, i, b);
+    }
+}
+
 // A tile's elements, scaled and with dropout, from LDS to x.
 template <typename TS>
 __device__ __forceinline__ void write_tile(const EmbedArgs &a, const Tiling &g, const Tile &w, const float *tile, TS *x,
@@ -113,7 +127,9 @@ __device__ __forceinline__ void write_tile(const EmbedArgs &a, const Tiling &g, 
 
 // A work-group's columns and `run` feature tiles one after the other: the next
 // tile's rows are on their way while this one is turned over and written.
-template <typename TS, int LV>
+// WHOLE: B is a multiple of 64 and x 16-byte aligned, the mask repeats after a
+// multiple of 8 if at all; DROP: with dropout (only told apart there).
+template <typename TS, int LV, bool WHOLE, bool DROP>
 __global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int run, bool aligned) {
     constexpr int PER = TILE / LV, LOADS = TILE * PER / NT;
     __shared__ float tile[TILE * PITCH];
@@ -158,7 +174,18 @@ __global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int ru
         w.ni = min(TILE, g.I - w.i0);
         if (n + 1 < last)
             fetch(w.i0 + TILE);
-        write_tile(a, g, w, tile, x, aligned);
+        if constexpr (WHOLE)
+            for_whole_groups(g, w, [&](long e, int i, int b) {
+                float o[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    o[k] = tile[(b + k) * PITCH + i] * a.scale;
+                if (DROP)
+                    drop8_whole(a.drop, e, o);
+                store8(x + e, o);
+            });
+        else
+            write_tile(a, g, w, tile, x, aligned);
         __syncthreads();
     }
 }
@@ -277,23 +304,8 @@ __device__ __forceinline__ void put(const EmbedGradArgs &a, float *p, float sum)
     *p = a.accumulate ? *p + sum * a.scale : sum * a.scale;
 }
 
-__global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sorted q, float *rows, bool aligned) {
-    __shared__ float tile[TILE * PITCH];
-    __shared__ float *dest[TILE];
-    __shared__ bool once[TILE];
-    const Tile w = tile_of(g, blockIdx.x);
-    if ((int)threadIdx.x < w.nb) {
-        const long p = (long)w.t * g.B + w.b0 + threadIdx.x;
-        const int v = a.tokens[p];
-        float *d = nullptr;
-        bool one = false;
-        if ((uint32_t)v < (uint32_t)a.V) {
-            one = q.start[v + 1] - q.start[v] == 1;
-            d = one ? a.dE + (long)v * a.I : rows + (long)q.rank[p] * a.I;
-        }
-        dest[threadIdx.x] = d;
-        once[threadIdx.x] = one;
-    }
+// A tile of dX, with dropout, into LDS.
+__device__ __forceinline__ void turn_in(const EmbedGradArgs &a, const Tiling &g, const Tile &w, float *tile, bool aligned) {
     for_groups(g, w, [&](long e, long lo, long hi, int i, int b, bool whole) {
         float f[8];
         if (whole && aligned) {
@@ -322,6 +334,39 @@ __global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sor
             }
         }
     });
+}
+
+// WHOLE, DROP as for the lookup.
+template <bool WHOLE, bool DROP>
+__global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sorted q, float *rows, bool aligned) {
+    __shared__ float tile[TILE * PITCH];
+    __shared__ float *dest[TILE];
+    __shared__ bool once[TILE];
+    const Tile w = tile_of(g, blockIdx.x);
+    if ((int)threadIdx.x < w.nb) {
+        const long p = (long)w.t * g.B + w.b0 + threadIdx.x;
+        const int v = a.tokens[p];
+        float *d = nullptr;
+        bool one = false;
+        if ((uint32_t)v < (uint32_t)a.V) {
+            one = q.start[v + 1] - q.start[v] == 1;
+            d = one ? a.dE + (long)v * a.I : rows + (long)q.rank[p] * a.I;
+        }
+        dest[threadIdx.x] = d;
+        once[threadIdx.x] = one;
+    }
+    if constexpr (WHOLE)
+        for_whole_groups(g, w, [&](long e, int i, int b) {
+            float f[8];
+            load8(a.dX + e, f);
+            if (DROP)
+                drop8_whole(a.drop, e, f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                tile[(b + k) * PITCH + i] = f[k];
+        });
+    else
+        turn_in(a, g, w, tile, aligned);
     __syncthreads();
     const int lane = threadIdx.x & 63;
     if (lane < w.ni)
@@ -478,11 +523,15 @@ hipError_t lookup(const EmbedArgs &a, hipStream_t s) {
     const long steps = (long)g.T * g.chunks;
     const int run = (int)std::max(1L, std::min(4L, steps * g.tiles / 2048));
     const dim3 grid((unsigned)(steps * ceil_div(g.tiles, run)));
-    const bool aligned = (uintptr_t)a.x % 16 == 0;
-    if ((uintptr_t)a.E % 16 == 0 && a.I % LV == 0)
-        hipLaunchKernelGGL((embed_kernel<TS, LV>), grid, dim3(NT), 0, s, a, g, run, aligned);
+    const bool aligned = (uintptr_t)a.x % 16 == 0, rows = (uintptr_t)a.E % 16 == 0 && a.I % LV == 0;
+    if (rows && aligned && a.B % TILE == 0 && a.drop.thr == 0)
+        hipLaunchKernelGGL((embed_kernel<TS, LV, true, false>), grid, dim3(NT), 0, s, a, g, run, aligned);
+    else if (rows && aligned && a.B % TILE == 0 && a.drop.period % 8 == 0)
+        hipLaunchKernelGGL((embed_kernel<TS, LV, true, true>), grid, dim3(NT), 0, s, a, g, run, aligned);
+    else if (rows)
+        hipLaunchKernelGGL((embed_kernel<TS, LV, false, true>), grid, dim3(NT), 0, s, a, g, run, aligned);
     else
-        hipLaunchKernelGGL((embed_kernel<TS, 1>), grid, dim3(NT), 0, s, a, g, run, aligned);
+        hipLaunchKernelGGL((embed_kernel<TS, 1, false, true>), grid, dim3(NT), 0, s, a, g, run, aligned);
     return hipGetLastError();
 }
 
@@ -525,8 +574,14 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
     const Tiling g = tiling_of(a.T, a.B, a.I);
     const long tiles = (long)g.T * g.chunks * g.tiles;
     const bool aligned = a.I % 4 == 0 && (uintptr_t)a.dE % 16 == 0;
-    hipLaunchKernelGGL(turn_kernel, dim3((unsigned)tiles), dim3(NT), 0, s, a, g, q, w.rows,
-                       (uintptr_t)a.dX % 16 == 0);
+    const dim3 grid((unsigned)tiles);
+    const bool from = (uintptr_t)a.dX % 16 == 0, whole = from && a.B % TILE == 0;
+    if (whole && a.drop.thr == 0)
+        hipLaunchKernelGGL((turn_kernel<true, false>), grid, dim3(NT), 0, s, a, g, q, w.rows, from);
+    else if (whole && a.drop.period % 8 == 0)
+        hipLaunchKernelGGL((turn_kernel<true, true>), grid, dim3(NT), 0, s, a, g, q, w.rows, from);
+    else
+        hipLaunchKernelGGL((turn_kernel<false, true>), grid, dim3(NT), 0, s, a, g, q, w.rows, from);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
     return group_of(N) == 16 ? walk<16>(a, q, w, N, aligned, s) : walk<64>(a, q, w, N, aligned, s);
