@@ -53,43 +53,44 @@ __device__ __forceinline__ Tile tile_of(const Tiling &g, long block) {
     return a;
 }
 
-// Calls f(e, lo, hi, i, b, whole) for the groups of eight elements e .. e + 7 (e a
-// multiple of 8) that cover a tile of the batch-last tensor, those in [lo, hi)
+// Calls f(e, lo, hi, i, b, whole) for the groups of VEC elements (16 bytes) from
+// e, a multiple of VEC, that cover a tile of the batch-last tensor, those in [lo, hi)
 // its own: element e + k is of column b + k, feature i while b + k < B, of the
-// next features from there.  b may be negative down to -7 in a group that
+// next features from there.  b may be negative, above -VEC, in a group that
 // begins before its piece.  `whole` holds for a group that is its tile's alone
-// and of one feature, which all are where B is a multiple of 8.
-template <class F>
+// and of one feature, which all are where B is a multiple of VEC.
+template <int VEC, class F>
 __device__ __forceinline__ void for_groups(const Tiling &g, const Tile &a, F &&f) {
     if (g.chunks == 1) {
         const long lo = ((long)a.t * g.I + a.i0) * g.B, hi = lo + (long)a.ni * g.B;
-        const long q0 = lo >> 3, q1 = (hi + 7) >> 3;
+        const long q0 = lo / VEC, q1 = (hi + VEC - 1) / VEC;
         for (long q = q0 + threadIdx.x; q < q1; q += NT) {
-            const int r = (int)(q * 8 - lo);
+            const int r = (int)(q * VEC - lo);
             const int i = r < 0 ? 0 : r / g.B, b = r - i * g.B;
-            f(q * 8, lo, hi, i, b, r >= 0 && q * 8 + 8 <= hi && b + 8 <= g.B);
+            f(q * VEC, lo, hi, i, b, r >= 0 && q * VEC + VEC <= hi && b + VEC <= g.B);
         }
     } else {
-        const int per = (a.nb + 7) / 8 + 1;
+        const int per = (a.nb + VEC - 1) / VEC + 1;
         for (int n = threadIdx.x; n < per * a.ni; n += NT) {
             const int i = n / per, j = n - i * per;
             const long lo = ((long)a.t * g.I + a.i0 + i) * g.B + a.b0, hi = lo + a.nb;
-            const long e = (lo >> 3) * 8 + j * 8;
+            const long e = lo / VEC * VEC + j * VEC;
             if (e < hi)
-                f(e, lo, hi, i, (int)(e - lo), e >= lo && e + 8 <= hi);
+                f(e, lo, hi, i, (int)(e - lo), e >= lo && e + VEC <= hi);
         }
     }
 }
 
-// Calls f(e, i, b) for the groups of a tile of 64 whole columns: eight to a
-// feature, each of that feature alone.
-template <class F>
+// Calls f(e, i, b) for the groups of a tile of 64 whole columns, each of one
+// feature alone.
+template <int VEC, class F>
 __device__ __forceinline__ void for_whole_groups(const Tiling &g, const Tile &a, F &&f) {
     const long lo = ((long)a.t * g.I + a.i0) * g.B + a.b0;
-    const int b = (threadIdx.x & 7) * 8;
+    constexpr int PER = TILE / VEC;
+    const int b = threadIdx.x % PER * VEC;
 #pragma unroll
-    for (int n = 0; n < TILE * 8 / NT; ++n) {
-        const int i = (threadIdx.x >> 3) + n * (NT / 8);
+    for (int n = 0; n < TILE * PER / NT; ++n) {
+        const int i = threadIdx.x / PER + n * (NT / PER);
         if (i < a.ni)
             f(lo + i * g.B + b, i, b);
     }
@@ -98,28 +99,29 @@ __device__ __forceinline__ void for_whole_groups(const Tiling &g, const Tile &a,
 // A tile's elements, scaled and with dropout, from LDS to x.
 template <typename TS>
 __device__ __forceinline__ void write_tile(const EmbedArgs &a, const Tiling &g, const Tile &w, const float *tile, TS *x,
-                                           bool aligned) {
-    for_groups(g, w, [&](long e, long lo, long hi, int i, int b, bool whole) {
-        float f[8];
-        if (whole && aligned) {
+                                           bool aligned, bool past) {
+    constexpr int VEC = vec_of<TS>();
+    for_groups<VEC>(g, w, [&](long e, long lo, long hi, int i, int b, bool whole) {
+        float f[VEC];
+        if (whole) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
+            for (int k = 0; k < VEC; ++k)
                 f[k] = tile[(b + k) * PITCH + i] * a.scale;
-            drop8(a.drop, e, f);
-            return store8(x + e, f);
-        }
+        } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const bool in = e + k >= lo && e + k < hi;
-            f[k] = in ? tile[b * PITCH + i] * a.scale : 0.f;
-            if (++b == g.B) {
-                b = 0;
-                ++i;
+            for (int k = 0; k < VEC; ++k) {
+                f[k] = e + k >= lo && e + k < hi ? tile[b * PITCH + i] * a.scale : 0.f;
+                if (++b == g.B) {
+                    b = 0;
+                    ++i;
+                }
             }
         }
-        drop8(a.drop, e, f);
+        drop_any<VEC>(a.drop, e, f);
+        if (aligned && e >= lo && e + VEC <= hi)
+            return store16(x + e, f, past);
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < VEC; ++k)
             if (e + k >= lo && e + k < hi)
                 st<TS>::store(x, e + k, f[k]);
     });
@@ -130,7 +132,7 @@ __device__ __forceinline__ void write_tile(const EmbedArgs &a, const Tiling &g, 
 // WHOLE: B is a multiple of 64 and x 16-byte aligned, the mask repeats after a
 // multiple of 8 if at all; DROP: with dropout (only told apart there).
 template <typename TS, int LV, bool WHOLE, bool DROP>
-__global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int run, bool aligned) {
+__global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int run, bool aligned, bool past) {
     constexpr int PER = TILE / LV, LOADS = TILE * PER / NT;
     __shared__ float tile[TILE * PITCH];
     const int runs = (g.tiles + run - 1) / run;
@@ -174,18 +176,19 @@ __global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int ru
         w.ni = min(TILE, g.I - w.i0);
         if (n + 1 < last)
             fetch(w.i0 + TILE);
-        if constexpr (WHOLE)
-            for_whole_groups(g, w, [&](long e, int i, int b) {
-                float o[8];
+        if constexpr (WHOLE) {
+            constexpr int VEC = vec_of<TS>();
+            for_whole_groups<VEC>(g, w, [&](long e, int i, int b) {
+                float o[VEC];
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < VEC; ++k)
                     o[k] = tile[(b + k) * PITCH + i] * a.scale;
                 if (DROP)
-                    drop8_whole(a.drop, e, o);
-                store8(x + e, o);
+                    drop_whole<VEC>(a.drop, e, o);
+                store16(x + e, o, past);
             });
-        else
-            write_tile(a, g, w, tile, x, aligned);
+        } else
+            write_tile(a, g, w, tile, x, aligned, past);
         __syncthreads();
     }
 }
@@ -306,26 +309,24 @@ __device__ __forceinline__ void put(const EmbedGradArgs &a, float *p, float sum)
 
 // A tile of dX, with dropout, into LDS.
 __device__ __forceinline__ void turn_in(const EmbedGradArgs &a, const Tiling &g, const Tile &w, float *tile, bool aligned) {
-    for_groups(g, w, [&](long e, long lo, long hi, int i, int b, bool whole) {
-        float f[8];
-        if (whole && aligned) {
-            load8(a.dX + e, f);
-            drop8(a.drop, e, f);
+    for_groups<4>(g, w, [&](long e, long lo, long hi, int i, int b, bool whole) {
+        float f[4];
+        if (aligned && e >= lo && e + 4 <= hi) {
+            vec<float, 4>::load(a.dX + e, f);
+        } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
+            for (int k = 0; k < 4; ++k)
+                f[k] = e + k >= lo && e + k < hi ? a.dX[e + k] : 0.f;
+        }
+        drop_any<4>(a.drop, e, f);
+        if (whole) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
                 tile[(b + k) * PITCH + i] = f[k];
             return;
         }
-        if (aligned && e >= lo && e + 8 <= hi) {
-            load8(a.dX + e, f);
-        } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                f[k] = e + k >= lo && e + k < hi ? a.dX[e + k] : 0.f;
-        }
-        drop8(a.drop, e, f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < 4; ++k) {
             if (e + k >= lo && e + k < hi)
                 tile[b * PITCH + i] = f[k];
             if (++b == g.B) {
@@ -356,13 +357,13 @@ __global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sor
         once[threadIdx.x] = one;
     }
     if constexpr (WHOLE)
-        for_whole_groups(g, w, [&](long e, int i, int b) {
-            float f[8];
-            load8(a.dX + e, f);
+        for_whole_groups<4>(g, w, [&](long e, int i, int b) {
+            float f[4];
+            vec<float, 4>::load(a.dX + e, f);
             if (DROP)
-                drop8_whole(a.drop, e, f);
+                drop_whole<4>(a.drop, e, f);
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
+            for (int k = 0; k < 4; ++k)
                 tile[(b + k) * PITCH + i] = f[k];
         });
     else
@@ -523,15 +524,16 @@ hipError_t lookup(const EmbedArgs &a, hipStream_t s) {
     const long steps = (long)g.T * g.chunks;
     const int run = (int)std::max(1L, std::min(4L, steps * g.tiles / 2048));
     const dim3 grid((unsigned)(steps * ceil_div(g.tiles, run)));
+    const bool past = (long)a.T * a.I * a.B * st<TS>::bytes >= STREAM_BYTES;
     const bool aligned = (uintptr_t)a.x % 16 == 0, rows = (uintptr_t)a.E % 16 == 0 && a.I % LV == 0;
     if (rows && aligned && a.B % TILE == 0 && a.drop.thr == 0)
-        hipLaunchKernelGGL((embed_kernel<TS, LV, true, false>), grid, dim3(NT), 0, s, a, g, run, aligned);
+        hipLaunchKernelGGL((embed_kernel<TS, LV, true, false>), grid, dim3(NT), 0, s, a, g, run, aligned, past);
     else if (rows && aligned && a.B % TILE == 0 && a.drop.period % 8 == 0)
-        hipLaunchKernelGGL((embed_kernel<TS, LV, true, true>), grid, dim3(NT), 0, s, a, g, run, aligned);
+        hipLaunchKernelGGL((embed_kernel<TS, LV, true, true>), grid, dim3(NT), 0, s, a, g, run, aligned, past);
     else if (rows)
-        hipLaunchKernelGGL((embed_kernel<TS, LV, false, true>), grid, dim3(NT), 0, s, a, g, run, aligned);
+        hipLaunchKernelGGL((embed_kernel<TS, LV, false, true>), grid, dim3(NT), 0, s, a, g, run, aligned, past);
     else
-        hipLaunchKernelGGL((embed_kernel<TS, 1, false, true>), grid, dim3(NT), 0, s, a, g, run, aligned);
+        hipLaunchKernelGGL((embed_kernel<TS, 1, false, true>), grid, dim3(NT), 0, s, a, g, run, aligned, past);
     return hipGetLastError();
 }
 

@@ -26,34 +26,35 @@ __device__ __forceinline__ void philox(uint64_t counter, uint32_t k0, uint32_t k
     out[3] = c3;
 }
 
-// f[k] scaled where the 16 bits number k of a counter's 128 reach the
-// threshold, else +0.  (Both halves of a word are compared in its high half.)
-__device__ __forceinline__ void drop_apply(const DropArgs &d, const uint32_t w[4], float *f) {
-    const uint32_t thr = d.thr << 16;
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-        f[k] = (k & 1 ? w[k >> 1] : w[k >> 1] << 16) >= thr ? f[k] * d.scale : 0.f;
-}
-
-// The same for masks that repeat, if at all, after a multiple of 8.
-__device__ __forceinline__ void drop8_whole(const DropArgs &d, long e, float *f) {
+// Dropout of the VEC elements e .. e + VEC - 1 (16 bytes of a type: VEC is 4
+// or 8, e a multiple of it) of a mask that repeats, if at all, after a
+// multiple of 8: +0 where dropped, whatever f holds.  Eight elements share a
+// counter.  Both halves of a word are compared in its high half.
+template <int VEC>
+__device__ __forceinline__ void drop_whole(const DropArgs &d, long e, float *f) {
     uint32_t w[4];
     const long m = d.period > 0 ? e % d.period : e;
     philox(d.counter + (uint64_t)(m >> 3), d.key0, d.key1, w);
-    drop_apply(d, w, f);
+    if (VEC == 4 && (m & 4)) {
+        w[0] = w[2];
+        w[1] = w[3];
+    }
+    const uint32_t thr = d.thr << 16;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+        f[k] = (k & 1 ? w[k >> 1] : w[k >> 1] << 16) >= thr ? f[k] * d.scale : 0.f;
 }
 
-// Dropout of the eight elements e .. e + 7 (e a multiple of 8): +0 where
-// dropped, whatever f holds.  One counter gives all eight, unless the mask
-// repeats after a length that is no multiple of 8.
-__device__ __forceinline__ void drop8(const DropArgs &d, long e, float *f) {
+// The same for any mask.
+template <int VEC>
+__device__ __forceinline__ void drop_any(const DropArgs &d, long e, float *f) {
     if (d.thr == 0)
         return;
     if ((d.period & 7) == 0)
-        return drop8_whole(d, e, f);
+        return drop_whole<VEC>(d, e, f);
     uint32_t w[4];
 #pragma unroll 1
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < VEC; ++k) {
         const long m = (e + k) % d.period;
         philox(d.counter + (uint64_t)(m >> 3), d.key0, d.key1, w);
         const int h = (int)(m & 7);

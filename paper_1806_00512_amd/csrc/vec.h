@@ -59,16 +59,29 @@ struct vec<bf16_t, 8> {
     }
 };
 
-// Eight elements from a 16-byte boundary.
-__device__ __forceinline__ void load8(const float *p, float *f) {
-    vec<float, 4>::load(p, f);
-    vec<float, 4>::load(p + 4, f + 4);
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes that go past the caches' usual order of eviction, for a tensor too
+// large for whoever reads it next to find it there.
+__device__ __forceinline__ void stream(float *p, const float *f) {
+    __builtin_nontemporal_store(f32x4{f[0], f[1], f[2], f[3]}, (f32x4 *)p);
 }
-__device__ __forceinline__ void load8(const bf16_t *p, float *f) { vec<bf16_t, 8>::load(p, f); }
-__device__ __forceinline__ void store8(float *p, const float *f) {
-    vec<float, 4>::store(p, f);
-    vec<float, 4>::store(p + 4, f + 4);
+__device__ __forceinline__ void stream(bf16_t *p, const float *f) {
+    __builtin_nontemporal_store(u32x4{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]),
+                                      pack_bf16(f[6], f[7])},
+                                (u32x4 *)p);
 }
-__device__ __forceinline__ void store8(bf16_t *p, const float *f) { vec<bf16_t, 8>::store(p, f); }
+template <typename TS>
+__device__ __forceinline__ void store16(TS *p, const float *f, bool past) {
+    if (past)
+        stream(p, f);
+    else
+        vec<TS, vec_of<TS>()>::store(p, f);
+}
+
+// Outputs from this size on are streamed: no L2 (4 MB for each of eight XCDs)
+// keeps them for their reader, and their lines do not push out what this
+// kernel reads again.
+constexpr long STREAM_BYTES = 32L << 20;
 
 } // namespace lstmss
