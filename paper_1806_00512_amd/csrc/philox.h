@@ -7,15 +7,20 @@
 
 namespace lstmss {
 
+// One instruction on gfx950 (truth table of a ^ b ^ c).
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+    return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
+}
+
 // The 128 bits of one counter: ten rounds of two 32 x 32 -> 64 products.
 __device__ __forceinline__ void philox(uint64_t counter, uint32_t k0, uint32_t k1, uint32_t out[4]) {
     uint32_t c0 = (uint32_t)counter, c1 = (uint32_t)(counter >> 32), c2 = 0, c3 = 0;
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = (uint64_t)0xD2511F53u * c0, b = (uint64_t)0xCD9E8D57u * c2;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c0 = xor3((uint32_t)(b >> 32), c1, k0);
         c1 = (uint32_t)b;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c2 = xor3((uint32_t)(a >> 32), c3, k1);
         c3 = (uint32_t)a;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
