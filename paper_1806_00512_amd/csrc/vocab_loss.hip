@@ -5,8 +5,11 @@
 //   dL/dx_v = dlogp * ([v = y] - exp(x_v - lse)),  lse = m + log s
 //
 // Three kernels: partial (m, s) of every column over a chunk of rows; the
-// per-token terms (the chunks' joined (m, s), logp, the loss, dlogp); the
-// gradient.  A step's logits are V * B elements in one piece, columns
+// per-token terms (the chunks' joined (m, s), logp, loss term, dlogp); the
+// gradient, one of whose work-groups also sums the loss.  The gradient's
+// work-groups go through the logits from the end, where the first kernel left
+// off: what of them is still in the last-level cache need not come from memory
+// again.  A step's logits are V * B elements in one piece, columns
 // fastest, so a thread that walks a piece in strides of whole rows keeps its
 // columns: their running (m, s), or their (lse, dlogp), stay in registers,
 // whatever B is.
@@ -79,6 +82,7 @@ struct Cut {
     int rows, chunks;  // rows of a chunk, chunks of a step
     int lanes;         // FLAT: threads at work; WIDE: 0
     int windows;       // WIDE: windows of 64 * VEC columns
+    bool past;         // the gradient is streamed
     int mis;           // elements from the 16-byte boundary before the logits to their start
 };
 
@@ -224,93 +228,128 @@ struct Coef {
     float lse, p;
 };
 
-// Four threads join a token's chunks; one of them does its terms in fp64.
+// 16 tokens to a work-group, 16 threads to a token: they join its chunks, and
+// one of them does its terms in fp64, on operands read while the chunks were.
+constexpr int TOKENS = 16;
+
 __global__ __launch_bounds__(NT) void token_kernel(LossArgs a, int chunks, const Stat *stat, Coef *coef, float *dtarget,
                                                    double *part) {
-    __shared__ Stat join[4][64];
-    __shared__ double red[64];
-    const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
-    const long N = (long)a.T * a.B, n = blockIdx.x * 64L + lane;
+    constexpr int SUBS = NT / TOKENS, U = 4;
+    __shared__ Stat join[NT / 64][TOKENS];
+    const int j = threadIdx.x % TOKENS, sub = threadIdx.x / TOKENS;
+    const long N = (long)a.T * a.B, n = (long)blockIdx.x * TOKENS + j;
     const int t = (int)(n / a.B), b = (int)(n - (long)t * a.B);
+    int y = -1;
+    float x = 0.f, w = 1.f, old = 0.f, ref = 0.f, adv = 0.f;
+    if (sub == 0 && n < N) {
+        y = a.targets[n];
+        if (a.weights)
+            w = a.weights[n];
+        if (a.old_logp)
+            old = a.old_logp[n];
+        if (a.ref_logp)
+            ref = a.ref_logp[n];
+        if (a.adv)
+            adv = a.adv[n];
+        if ((uint32_t)y < (uint32_t)a.V) {
+            const long at = ((long)t * a.V + y) * a.B + b;
+            x = a.bf16 ? st<bf16_t>::load((const bf16_t *)a.logits, at) : ((const float *)a.logits)[at];
+        }
+    }
     Stat q = {-FLT_MAX, 0.f};
     if (n < N)
-        for (int c = row; c < chunks; c += 4)
-            q = stat_join(q, stat[((long)t * chunks + c) * a.B + b]);
-    join[row][lane] = q;
+        for (int c = sub; c < chunks; c += SUBS * U) {
+            Stat r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                r[u] = c + u * SUBS < chunks ? stat[((long)t * chunks + c + u * SUBS) * a.B + b] : Stat{-FLT_MAX, 0.f};
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                q = stat_join(q, r[u]);
+        }
+#pragma unroll
+    for (int m = TOKENS; m < 64; m <<= 1)
+        q = stat_join(q, Stat{__shfl_xor(q.m, m, 64), __shfl_xor(q.s, m, 64)});
+    if ((threadIdx.x & 63) < TOKENS)
+        join[threadIdx.x >> 6][j] = q;
     __syncthreads();
-    if (row == 0) {
-        double term = 0.0;
-        if (n < N) {
-            for (int r = 1; r < 4; ++r)
-                q = stat_join(q, join[r][lane]);
-            const int y = a.targets[n];
-            const double w = a.weights ? (double)a.weights[n] : 1.0;
-            double lp = 0.0, g = 0.0;
-            Coef c = {0.f, 0.f};
-            float dt = 0.f;
-            if ((uint32_t)y < (uint32_t)a.V && w != 0.0) {
-                const long at = ((long)t * a.V + y) * a.B + b;
-                const float x = a.bf16 ? st<bf16_t>::load((const bf16_t *)a.logits, at) : ((const float *)a.logits)[at];
-                const double ls = log((double)q.s), lse = (double)q.m + ls;
-                lp = ((double)x - (double)q.m) - ls;
-                if (a.mode == LOSS_XENT) {
-                    term = -lp;
-                    g = -1.0;
-                } else if (a.mode == LOSS_POLICY) {
-                    const double A = a.adv[n];
-                    const double r = a.old_logp ? exp(lp - (double)a.old_logp[n]) : 1.0;
-                    const double cl = fmin(fmax(r, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high);
-                    const double gain = r * A, held = cl * A;
-                    const bool open = gain <= held || gain != gain;
-                    term = -(open ? gain : held);
-                    g = open ? -gain : 0.0;
-                    if (a.ref_logp) {
-                        const double d = (double)a.ref_logp[n] - lp, e = expm1(d);
-                        term += (double)a.kl * (e - d);
-                        g -= (double)a.kl * e;
-                    }
-                }
-                term *= w * (double)a.scale;
-                g *= w * (double)a.scale;
-                if (g != 0.0) {
-                    c.lse = (float)lse;
-                    c.p = (float)(-g * exp((double)c.lse - lse));
-                    dt = (float)(-g * expm1(lp));
+    if (threadIdx.x >= TOKENS)
+        return;
+    for (int r = 1; r < NT / 64; ++r)
+        q = stat_join(q, join[r][j]);
+    double term = 0.0;
+    if (n < N) {
+        double lp = 0.0, g = 0.0;
+        Coef c = {0.f, 0.f};
+        float dt = 0.f;
+        if ((uint32_t)y < (uint32_t)a.V && w != 0.f) {
+            const double ls = log((double)q.s), lse = (double)q.m + ls;
+            lp = ((double)x - (double)q.m) - ls;
+            if (a.mode == LOSS_XENT) {
+                term = -lp;
+                g = -1.0;
+            } else if (a.mode == LOSS_POLICY) {
+                const double A = adv;
+                const double r = a.old_logp ? exp(lp - (double)old) : 1.0;
+                const double cl = fmin(fmax(r, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high);
+                const double gain = r * A, held = cl * A;
+                const bool open = gain <= held || gain != gain;
+                term = -(open ? gain : held);
+                g = open ? -gain : 0.0;
+                if (a.ref_logp) {
+                    const double d = (double)ref - lp, e = expm1(d);
+                    term += (double)a.kl * (e - d);
+                    g -= (double)a.kl * e;
                 }
             }
-            if (a.logp)
-                a.logp[n] = (float)lp;
-            coef[n] = c;
-            dtarget[n] = dt;
+            term *= (double)w * (double)a.scale;
+            g *= (double)w * (double)a.scale;
+            if (g != 0.0) {
+                // lse's rounding is made good in p, to first order (its square is below 2^-48)
+                c.lse = (float)lse;
+                c.p = (float)(-g * (1.0 + ((double)c.lse - lse)));
+                dt = (float)(-g * expm1(lp));
+            }
         }
-        red[lane] = term;
+        if (a.logp)
+            a.logp[n] = (float)lp;
+        coef[n] = c;
+        dtarget[n] = dt;
     }
-    __syncthreads();
-    for (int w = 32; w >= 1; w >>= 1) {
-        if ((int)threadIdx.x < w)
-            red[threadIdx.x] += red[threadIdx.x + w];
-        __syncthreads();
-    }
+#pragma unroll
+    for (int m = TOKENS / 2; m >= 1; m >>= 1)
+        term += __shfl_xor(term, m, 64);
     if (threadIdx.x == 0)
-        part[blockIdx.x] = red[0];
+        part[blockIdx.x] = term;
 }
 
-// The token kernel's partial sums in a fixed order.
-__global__ __launch_bounds__(NT) void loss_sum_kernel(const double *part, int n, float *loss) {
-    __shared__ double red[NT];
+// The loss: the token kernel's partial sums in a fixed order, by one
+// work-group.
+struct LossOut {
+    const double *part;
+    int parts;
+    float *loss; // NULL: not asked for
+};
+
+__device__ __forceinline__ void loss_sum(const LossOut &o) {
+    __shared__ double red[NT / 64];
     double sum = 0.0;
-    for (int i = threadIdx.x; i < n; i += NT)
-        sum += part[i];
-    red[threadIdx.x] = sum;
+    for (int i = threadIdx.x; i < o.parts; i += blockDim.x)
+        sum += o.part[i];
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1)
+        sum += __shfl_xor(sum, m, 64);
+    if ((threadIdx.x & 63) == 0)
+        red[threadIdx.x >> 6] = sum;
     __syncthreads();
-    for (int w = NT / 2; w >= 1; w >>= 1) {
-        if ((int)threadIdx.x < w)
-            red[threadIdx.x] += red[threadIdx.x + w];
-        __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < (int)blockDim.x / 64; ++w)
+            sum += red[w];
+        *o.loss = (float)sum;
     }
-    if (threadIdx.x == 0)
-        *loss = (float)red[0];
 }
+
+__global__ __launch_bounds__(NT) void loss_sum_kernel(LossOut o) { loss_sum(o); }
 
 __device__ __forceinline__ float grad_of(float x, Coef c) { return c.p * __expf(fminf(x - c.lse, 1.f)); }
 
@@ -329,9 +368,11 @@ __device__ __forceinline__ void grad_targets(const Cut &g, const Piece &p, int b
 
 template <typename TS, int VEC>
 __global__ __launch_bounds__(NT) void grad_flat_kernel(Cut g, const TS *logits, TS *dlogits, const int32_t *targets,
-                                                       const Coef *coef, const float *dtarget) {
+                                                       const Coef *coef, const float *dtarget, LossOut o) {
     constexpr int U = 4;
-    const Piece p = piece_of(g, blockIdx.x);
+    if (o.loss && blockIdx.x == 0)
+        loss_sum(o);
+    const Piece p = piece_of(g, gridDim.x - 1 - blockIdx.x);
     const TS *x = logits - g.mis;
     TS *y = dlogits - g.mis;
     const long first = p.lo / VEC * VEC;
@@ -373,7 +414,10 @@ __global__ __launch_bounds__(NT) void grad_flat_kernel(Cut g, const TS *logits, 
 #pragma unroll
                 for (int k = 0; k < VEC; ++k)
                     f[u][k] = grad_of(f[u][k], c[k]);
-                vec<TS, VEC>::store(y + at + u * step, f[u]);
+                if constexpr (VEC > 1)
+                    store16(y + at + u * step, f[u], g.past);
+                else
+                    vec<TS, VEC>::store(y + at + u * step, f[u]);
             }
         }
         while (at < p.hi)
@@ -385,11 +429,13 @@ __global__ __launch_bounds__(NT) void grad_flat_kernel(Cut g, const TS *logits, 
 
 template <typename TS, int VEC>
 __global__ __launch_bounds__(NT) void grad_wide_kernel(Cut g, const TS *logits, TS *dlogits, const int32_t *targets,
-                                                       const Coef *coef, const float *dtarget) {
+                                                       const Coef *coef, const float *dtarget, LossOut o) {
     constexpr int U = 4;
-    const Piece p = piece_of(g, blockIdx.x / g.windows);
+    if (o.loss && blockIdx.x == 0)
+        loss_sum(o);
+    const Piece p = piece_of(g, (gridDim.x - 1 - blockIdx.x) / g.windows);
     const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
-    const int w0 = (int)(blockIdx.x % g.windows) * 64 * VEC, b = w0 + lane * VEC;
+    const int w0 = (int)((gridDim.x - 1 - blockIdx.x) % g.windows) * 64 * VEC, b = w0 + lane * VEC;
     if (b < g.B) {
         Coef c[VEC];
 #pragma unroll
@@ -407,7 +453,10 @@ __global__ __launch_bounds__(NT) void grad_wide_kernel(Cut g, const TS *logits, 
 #pragma unroll
                 for (int k = 0; k < VEC; ++k)
                     f[u][k] = grad_of(f[u][k], c[k]);
-                vec<TS, VEC>::store(dlogits + s0 + (long)(v + u * 4) * g.B, f[u]);
+                if constexpr (VEC > 1)
+                    store16(dlogits + s0 + (long)(v + u * 4) * g.B, f[u], g.past);
+                else
+                    vec<TS, VEC>::store(dlogits + s0 + (long)(v + u * 4) * g.B, f[u]);
             }
         }
         for (; v < p.v1; v += 4) {
@@ -430,7 +479,7 @@ constexpr long GROUPS = 2048, BYTES = 16384;
 
 // The cut for vectors of VEC elements.
 Cut cut_of(int T, int B, int V, int es, int VEC, int mis) {
-    Cut g = {T, V, B, V, 1, 0, 1, mis};
+    Cut g = {T, V, B, V, 1, 0, 1, (long)T * V * B * es >= STREAM_BYTES, mis};
     const int repeat = B / std::gcd(B, VEC);
     if (repeat <= NT)
         g.lanes = NT / repeat * repeat;
@@ -457,7 +506,7 @@ LossWs layout(void *ws, int T, int B, size_t chunks) {
     const size_t N = (size_t)T * B;
     char *p = (char *)ws;
     LossWs w;
-    w.parts = (int)((N + 63) / 64);
+    w.parts = (int)((N + TOKENS - 1) / TOKENS);
     size_t at = 0;
     w.stat = (Stat *)(p + at);
     at += align256(N * chunks * sizeof(Stat));
@@ -488,17 +537,18 @@ hipError_t run(const LossArgs &a, Cut g, const LossWs &w, hipStream_t s) {
                        w.part);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
-    if (a.loss) {
-        hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(NT), 0, s, w.part, w.parts, a.loss);
-        if ((e = hipGetLastError()) != hipSuccess)
-            return e;
+    const LossOut o = {w.part, w.parts, a.loss};
+    if (!y) {
+        if (a.loss)
+            hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(NT), 0, s, o);
+        return hipGetLastError();
     }
-    if (!y)
-        return hipSuccess;
     if (g.lanes)
-        hipLaunchKernelGGL((grad_flat_kernel<TS, VEC>), dim3(grid), dim3(flat), 0, s, g, x, y, a.targets, w.coef, w.dtarget);
+        hipLaunchKernelGGL((grad_flat_kernel<TS, VEC>), dim3(grid), dim3(flat), 0, s, g, x, y, a.targets, w.coef,
+                           w.dtarget, o);
     else
-        hipLaunchKernelGGL((grad_wide_kernel<TS, VEC>), dim3(grid), dim3(NT), 0, s, g, x, y, a.targets, w.coef, w.dtarget);
+        hipLaunchKernelGGL((grad_wide_kernel<TS, VEC>), dim3(grid), dim3(NT), 0, s, g, x, y, a.targets, w.coef,
+                           w.dtarget, o);
     return hipGetLastError();
 }
 
