@@ -71,6 +71,21 @@ __device__ __forceinline__ void stream(bf16_t *p, const float *f) {
                                       pack_bf16(f[6], f[7])},
                                 (u32x4 *)p);
 }
+__device__ __forceinline__ void load_past(const float *p, float *f) {
+    const f32x4 v = __builtin_nontemporal_load((const f32x4 *)p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        f[k] = v[k];
+}
+__device__ __forceinline__ void load_past(const bf16_t *p, float *f) {
+    const u32x4 v = __builtin_nontemporal_load((const u32x4 *)p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        f[2 * k] = __uint_as_float(v[k] << 16);
+        f[2 * k + 1] = __uint_as_float(v[k] & 0xffff0000u);
+    }
+}
+
 template <typename TS>
 __device__ __forceinline__ void store16(TS *p, const float *f, bool past) {
     if (past)
