@@ -493,9 +493,13 @@ __global__ __launch_bounds__(NT) void grad_wide_kernel(Cut g, const TS *logits, 
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// A work-group's share of a step: `bytes` or more of logits, and no more
-// groups than `groups` over all steps.
-constexpr long GROUPS = 2048, BYTES = 16384;
+// A work-group's share of a step: PIECE bytes of logits, in the first kernel
+// more where that makes over GROUPS work-groups (each leaves (m, s) of every
+// column), and whole multiples of PIECE where a number of rows comes to that.
+// The gradient's work-groups leave nothing, so finer ones only end more evenly.
+// 50 x 32000 x 128 bf16, loss and gradient, us by the gradient's piece: 32 KB 205,
+// 16 KB 200, 8 KB 238, 4 KB 310; of about 25 KB, not on such boundaries, 223.
+constexpr long PIECE = 16384, GROUPS = 2048, GRAD_GROUPS = 1L << 22;
 
 // What of the logits the first kernel leaves in the last-level cache (256 MB)
 // for the gradient: the last of them; what comes before is read past it, which
@@ -504,7 +508,7 @@ constexpr long GROUPS = 2048, BYTES = 16384;
 constexpr long KEEP_BYTES = 224L << 20;
 
 // The cut for vectors of VEC elements.
-Cut cut_of(int T, int B, int V, int es, int VEC, int mis) {
+Cut cut_of(int T, int B, int V, int es, int VEC, int mis, long groups) {
     Cut g = {T, V, B, V, 1, 0, 1, (long)T * V * B * es >= STREAM_BYTES, 0, mis};
     const int repeat = B / std::gcd(B, VEC);
     if (repeat <= NT)
@@ -512,9 +516,12 @@ Cut cut_of(int T, int B, int V, int es, int VEC, int mis) {
     else
         g.windows = (int)ceil_div(B, 64 * VEC);
     const long across = (long)T * g.windows;
-    const long by_groups = ceil_div(GROUPS, across), by_bytes = (long)V * B * es / g.windows / BYTES;
+    const long by_groups = ceil_div(groups, across), by_bytes = (long)V * B * es / g.windows / PIECE;
     long chunks = std::max(1L, std::min(std::min(by_groups, by_bytes), (long)V));
     g.rows = (int)ceil_div(V, chunks);
+    const long even = PIECE / std::gcd(PIECE, (long)B * es);
+    if (even <= g.rows)
+        g.rows = (int)(ceil_div(g.rows, even) * even);
     g.chunks = (int)ceil_div(V, g.rows);
     const long blocks = across * g.chunks, keep = KEEP_BYTES / std::max(1L, (long)T * V * B * es / blocks);
     g.first = (unsigned)std::max(0L, blocks - keep);
@@ -571,11 +578,13 @@ hipError_t run(const LossArgs &a, Cut g, const LossWs &w, hipStream_t s) {
             hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(NT), 0, s, o);
         return hipGetLastError();
     }
+    g = cut_of(g.T, g.B, g.V, st<TS>::bytes, VEC, g.mis, GRAD_GROUPS);
+    const unsigned pieces = (unsigned)((long)g.T * g.chunks * g.windows);
     if (g.lanes)
-        hipLaunchKernelGGL((grad_flat_kernel<TS, VEC>), dim3(grid), dim3(flat), 0, s, g, x, y, a.targets, w.coef,
+        hipLaunchKernelGGL((grad_flat_kernel<TS, VEC>), dim3(pieces), dim3(flat), 0, s, g, x, y, a.targets, w.coef,
                            w.dtarget, o);
     else
-        hipLaunchKernelGGL((grad_wide_kernel<TS, VEC>), dim3(grid), dim3(NT), 0, s, g, x, y, a.targets, w.coef,
+        hipLaunchKernelGGL((grad_wide_kernel<TS, VEC>), dim3(pieces), dim3(NT), 0, s, g, x, y, a.targets, w.coef,
                            w.dtarget, o);
     return hipGetLastError();
 }
@@ -587,10 +596,10 @@ hipError_t dispatch(const LossArgs &a, hipStream_t s) {
     constexpr int VEC = vec_of<TS>(), ES = st<TS>::bytes;
     const int mis = (int)((uintptr_t)a.logits / ES % VEC);
     const bool alike = !a.dlogits || (int)((uintptr_t)a.dlogits / ES % VEC) == mis;
-    Cut g = cut_of(a.T, a.B, a.V, ES, VEC, mis);
+    Cut g = cut_of(a.T, a.B, a.V, ES, VEC, mis, GROUPS);
     if (alike && (g.lanes || (mis == 0 && a.B % VEC == 0)))
         return run<TS, VEC>(a, g, layout(a.ws, a.T, a.B, g.chunks), s);
-    g = cut_of(a.T, a.B, a.V, ES, 1, 0);
+    g = cut_of(a.T, a.B, a.V, ES, 1, 0, GROUPS);
     return run<TS, 1>(a, g, layout(a.ws, a.T, a.B, g.chunks), s);
 }
 
@@ -599,7 +608,7 @@ hipError_t dispatch(const LossArgs &a, hipStream_t s) {
 // For either cut: where the tensors start is not known here.
 size_t loss_ws(int T, int B, int V, bool bf16) {
     const int es = bf16 ? 2 : 4;
-    const int a = cut_of(T, B, V, es, 16 / es, 0).chunks, b = cut_of(T, B, V, es, 1, 0).chunks;
+    const int a = cut_of(T, B, V, es, 16 / es, 0, GROUPS).chunks, b = cut_of(T, B, V, es, 1, 0, GROUPS).chunks;
     return layout(nullptr, T, B, (size_t)std::max(a, b)).bytes;
 }
 
