@@ -197,7 +197,7 @@ __global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int ru
 
 constexpr int SORT_NT = 1024, SORT_WAVES = SORT_NT / 64, SORT_MOST = 512;
 
-constexpr long FILL = 65536; // elements that a work-group zeroes
+constexpr long FILL = 16384; // elements that a work-group zeroes
 
 __device__ __forceinline__ void zero_fill(float *p, long i0, long i1) {
     // whole vectors between the first and the last 16-byte boundary, the rest singly
@@ -218,7 +218,8 @@ __device__ __forceinline__ void zero_fill(float *p, long i0, long i1) {
 // The work-groups from `sorters` on zero dE meanwhile, which the sort leaves
 // the memory free for: rows in use are written after this launch.
 __global__ __launch_bounds__(SORT_NT) void sort_kernel(const int32_t *tokens, int N, int V, int R, int32_t *rank,
-                                                       int32_t *key, int32_t *start, int sorters, float *dE, long size) {
+                                                       int32_t *order, int32_t *key, int32_t *start, int sorters,
+                                                       float *dE, long size) {
     if ((int)blockIdx.x >= sorters) {
         const long i0 = (long)(blockIdx.x - sorters) * FILL, i1 = min(size, i0 + FILL);
         return zero_fill(dE, i0, i1);
@@ -291,6 +292,7 @@ __global__ __launch_bounds__(SORT_NT) void sort_kernel(const int32_t *tokens, in
         if (in) {
             const int first = next[k], r = first + __popcll(same & below);
             rank[p] = r;
+            order[r] = p;
             key[r] = lo + (int)k;
             if ((same & below) == 0)
                 next[k] = first + __popcll(same);
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(SORT_NT) void sort_kernel(const int32_t *tokens, in
 
 // A token's range of ranks.
 struct Sorted {
-    const int32_t *rank, *key, *start; // [N], [N], [V + 1]
+    const int32_t *rank, *order, *key, *start; // [N], [N], [N], [V + 1]
 };
 
 __device__ __forceinline__ void put(const EmbedGradArgs &a, float *p, float sum) {
@@ -337,13 +339,31 @@ __device__ __forceinline__ void turn_in(const EmbedGradArgs &a, const Tiling &g,
     });
 }
 
-// WHOLE, DROP as for the lookup.
+// WHOLE, DROP as for the lookup.  A work-group's columns and `run` feature
+// tiles one after the other, the next tile's elements on their way meanwhile
+// (WHOLE).
 template <bool WHOLE, bool DROP>
-__global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sorted q, float *rows, bool aligned) {
+__global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sorted q, float *rows, int run, bool aligned) {
+    constexpr int PER = TILE / 4, LOADS = TILE * PER / NT;
     __shared__ float tile[TILE * PITCH];
     __shared__ float *dest[TILE];
     __shared__ bool once[TILE];
-    const Tile w = tile_of(g, blockIdx.x);
+    const int runs = (g.tiles + run - 1) / run;
+    const int part = blockIdx.x % runs, last = min(g.tiles, (part + 1) * run);
+    Tile w = tile_of(g, (long)(blockIdx.x / runs) * g.tiles + part * run);
+    float f[LOADS][4];
+    const int b = threadIdx.x % PER * 4;
+    auto fetch = [&](int i0) {
+        const long lo = ((long)w.t * g.I + i0) * g.B + w.b0 + b;
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            const int i = threadIdx.x / PER + k * (NT / PER);
+            if (i0 + i < g.I)
+                load_past(a.dX + lo + i * g.B, f[k]);
+        }
+    };
+    if (WHOLE)
+        fetch(w.i0);
     if ((int)threadIdx.x < w.nb) {
         const long p = (long)w.t * g.B + w.b0 + threadIdx.x;
         const int v = a.tokens[p];
@@ -356,32 +376,41 @@ __global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sor
         dest[threadIdx.x] = d;
         once[threadIdx.x] = one;
     }
-    if constexpr (WHOLE)
-        for_whole_groups<4>(g, w, [&](long e, int i, int b) {
-            float f[4];
-            vec<float, 4>::load(a.dX + e, f);
-            if (DROP)
-                drop_whole<4>(a.drop, e, f);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                tile[(b + k) * PITCH + i] = f[k];
-        });
-    else
-        turn_in(a, g, w, tile, aligned);
-    __syncthreads();
     const int lane = threadIdx.x & 63;
-    if (lane < w.ni)
-        for (int b = threadIdx.x >> 6; b < w.nb; b += NT / 64) {
-            float *d = dest[b];
-            if (!d)
-                continue;
-            const float f = tile[b * PITCH + lane];
-            d += w.i0 + lane;
-            if (once[b])
-                put(a, d, f);
-            else
-                *d = f;
+    for (int n = part * run; n < last; ++n) {
+        w.i0 = n * TILE;
+        w.ni = min(TILE, g.I - w.i0);
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k) {
+                const int i = threadIdx.x / PER + k * (NT / PER);
+                if (i >= w.ni)
+                    continue;
+                if (DROP)
+                    drop_whole<4>(a.drop, ((long)w.t * g.I + w.i0 + i) * g.B + w.b0 + b, f[k]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    tile[(b + j) * PITCH + i] = f[k][j];
+            }
+        } else {
+            turn_in(a, g, w, tile, aligned);
         }
+        __syncthreads();
+        if (WHOLE && n + 1 < last)
+            fetch(w.i0 + TILE);
+        if (lane < w.ni)
+            for (int c = threadIdx.x >> 6; c < w.nb; c += NT / 64) {
+                float *d = dest[c];
+                if (!d)
+                    continue;
+                d += w.i0 + lane;
+                if (once[c])
+                    put(a, d, tile[c * PITCH + lane]);
+                else
+                    *d = tile[c * PITCH + lane];
+            }
+        __syncthreads();
+    }
 }
 
 // Rows [G q, G q + G) of the sorted rows, VEC features to a thread: the sums
@@ -476,6 +505,89 @@ __global__ __launch_bounds__(NT) void carry_kernel(EmbedGradArgs a, Sorted s, co
     put(a, a.dE + (long)v * a.I + i, sum_parts(first, carry + (long)q * 2 * a.I + i, last - q + 1, 2L * a.I));
 }
 
+// Few positions: a work-group takes FEW features of all of them into LDS and
+// sums there, a thread for each feature of a run; one launch instead of three.
+// us, Zipf tokens over 5000 rows, this kernel with 4 and 8 features against the
+// three launches: 992 positions, 1024 features 14.2, 15.7, 21.4; 2048 positions,
+// 1024 features 21.3, 22.3, 25.2, 2048 features 31.0, 24.1, 28.5, 4096 features
+// 50, 39, 36; 3968 positions, 1024 features 32, 40, 29.  So: 4 features while
+// that makes no more work-groups than CUs; not over 2048 positions or 2^22
+// elements.
+constexpr int FEW_NT = 1024, FEW_MOST = 2048, FEW_CUS = 256;
+constexpr long FEW_SIZE = 1L << 22;
+
+template <int FEW>
+constexpr size_t few_lds(int N) {
+    return (size_t)N * ((FEW + 1) * sizeof(float) + 2 * sizeof(uint16_t));
+}
+
+template <int FEW>
+__global__ __launch_bounds__(FEW_NT) void few_kernel(EmbedGradArgs a, Sorted q, int N, bool aligned) {
+    constexpr int FEW_PITCH = FEW + 1;
+    extern __shared__ float tile[];                             // [N][FEW_PITCH]
+    uint16_t *order = (uint16_t *)(tile + (long)N * FEW_PITCH); // [N] the sorted rows' positions
+    uint16_t *length = order + N;                               // [N] of the run that begins at a row, else 0
+    const int M = q.start[a.V];
+    for (int r = threadIdx.x; r < M; r += FEW_NT) {
+        const int v = q.key[r];
+        order[r] = (uint16_t)q.order[r];
+        length[r] = (uint16_t)(q.start[v] == r ? q.start[v + 1] - r : 0);
+    }
+    const int i0 = blockIdx.x * FEW, ni = min(FEW, a.I - i0), len = ni * a.B;
+    // groups of four elements that cover a step's ni * B, which lie in one piece
+    const int per = len / 4 + 2;
+    for (long n = threadIdx.x; n < (long)a.T * per; n += FEW_NT) {
+        const int t = (int)(n / per), j = (int)(n - (long)t * per);
+        const long lo = ((long)t * a.I + i0) * a.B, hi = lo + len, e = lo / 4 * 4 + (long)j * 4;
+        if (e >= hi)
+            continue;
+        float f[4];
+        if (aligned && e >= lo && e + 4 <= hi) {
+            vec<float, 4>::load(a.dX + e, f);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                f[k] = e + k >= lo && e + k < hi ? a.dX[e + k] : 0.f;
+        }
+        drop_any<4>(a.drop, e, f);
+        const int r = (int)(e - lo);
+        int i = r < 0 ? 0 : r / a.B, b = r - i * a.B;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (e + k >= lo && e + k < hi)
+                tile[(t * a.B + b) * FEW_PITCH + i] = f[k];
+            if (++b == a.B) {
+                b = 0;
+                ++i;
+            }
+        }
+    }
+    __syncthreads();
+    const int i = threadIdx.x % FEW;
+    if (i >= ni)
+        return;
+    for (int r = threadIdx.x / FEW; r < M; r += FEW_NT / FEW) {
+        const int n = length[r];
+        if (n == 0)
+            continue;
+        const int v = q.key[r];
+        float sum = 0.f;
+        int k = 0;
+        for (; k + 8 <= n; k += 8) {
+            float f[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                f[u] = tile[order[r + k + u] * FEW_PITCH + i];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                sum += f[u];
+        }
+        for (; k < n; ++k)
+            sum += tile[order[r + k] * FEW_PITCH + i];
+        put(a, a.dE + (long)v * a.I + i0 + i, sum);
+    }
+}
+
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 Tiling tiling_of(int T, int B, int I) {
@@ -493,7 +605,7 @@ Tiling tiling_of(int T, int B, int I) {
 int group_of(int N) { return N < 32768 ? 16 : 64; }
 
 struct GradWs {
-    int32_t *rank, *key, *start;
+    int32_t *rank, *order, *key, *start;
     float *rows, *carry;
     size_t bytes;
 };
@@ -508,6 +620,7 @@ GradWs layout(void *ws, int N, int I, int V) {
         return r;
     };
     w.rank = (int32_t *)take((size_t)N * 4);
+    w.order = (int32_t *)take((size_t)N * 4);
     w.key = (int32_t *)take((size_t)N * 4);
     w.start = (int32_t *)take(((size_t)V + 1) * 4);
     w.rows = (float *)take((size_t)N * I * 4);
@@ -565,25 +678,35 @@ size_t embed_grad_ws(int T, int B, int I, int V) { return layout(nullptr, T * B,
 hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
     const int N = a.T * a.B;
     const GradWs w = layout(a.ws, N, a.I, a.V);
-    const Sorted q = {w.rank, w.key, w.start};
+    const Sorted q = {w.rank, w.order, w.key, w.start};
     const int R = std::min(SORT_MOST, (int)ceil_div(a.V, 256));
     const long size = (long)a.V * a.I, sorters = ceil_div(a.V, R), fills = a.accumulate ? 0 : ceil_div(size, FILL);
     hipLaunchKernelGGL(sort_kernel, dim3((unsigned)(sorters + fills)), dim3(SORT_NT), 0, s, a.tokens, N, a.V, R, w.rank,
-                       w.key, w.start, (int)sorters, a.dE, size);
+                       w.order, w.key, w.start, (int)sorters, a.dE, size);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
+    const bool from = (uintptr_t)a.dX % 16 == 0;
+    if (N <= FEW_MOST && (long)N * a.I <= FEW_SIZE) {
+        if (a.I <= 4 * FEW_CUS)
+            hipLaunchKernelGGL(few_kernel<4>, dim3((unsigned)ceil_div(a.I, 4)), dim3(FEW_NT), few_lds<4>(N), s, a, q, N, from);
+        else
+            hipLaunchKernelGGL(few_kernel<8>, dim3((unsigned)ceil_div(a.I, 8)), dim3(FEW_NT), few_lds<8>(N), s, a, q, N, from);
+        return hipGetLastError();
+    }
     const Tiling g = tiling_of(a.T, a.B, a.I);
-    const long tiles = (long)g.T * g.chunks * g.tiles;
+    // runs of up to four tiles while 2048 work-groups (eight on a CU) are left
+    const long steps = (long)g.T * g.chunks;
+    const int run = (int)std::max(1L, std::min(4L, steps * g.tiles / 2048));
     const bool aligned = a.I % 4 == 0 && (uintptr_t)a.dE % 16 == 0;
-    const dim3 grid((unsigned)tiles);
-    const bool from = (uintptr_t)a.dX % 16 == 0, whole = from && a.B % TILE == 0;
+    const dim3 grid((unsigned)(steps * ceil_div(g.tiles, run)));
+    const bool whole = from && a.B % TILE == 0;
     if (whole && a.drop.thr == 0)
-        hipLaunchKernelGGL((turn_kernel<true, false>), grid, dim3(NT), 0, s, a, g, q, w.rows, from);
+        hipLaunchKernelGGL((turn_kernel<true, false>), grid, dim3(NT), 0, s, a, g, q, w.rows, run, from);
     else if (whole && a.drop.period % 8 == 0)
-        hipLaunchKernelGGL((turn_kernel<true, true>), grid, dim3(NT), 0, s, a, g, q, w.rows, from);
+        hipLaunchKernelGGL((turn_kernel<true, true>), grid, dim3(NT), 0, s, a, g, q, w.rows, run, from);
     else
-        hipLaunchKernelGGL((turn_kernel<false, true>), grid, dim3(NT), 0, s, a, g, q, w.rows, from);
+        hipLaunchKernelGGL((turn_kernel<false, true>), grid, dim3(NT), 0, s, a, g, q, w.rows, run, from);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
     return group_of(N) == 16 ? walk<16>(a, q, w, N, aligned, s) : walk<64>(a, q, w, N, aligned, s);
