@@ -595,9 +595,10 @@ def _drop_ptr(d):
     return ctypes.byref(d)
 
 
-# The current stream of a GPU as a plain number; torch.cuda.current_stream()
-# builds an object around it, which takes as long as half a kernel launch.
+# The current GPU, and its current stream as a plain number: torch.cuda.current_stream()
+# builds an object around it, which takes as long as a kernel launch.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_gpu = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _on(first, name, stream):
@@ -607,7 +608,7 @@ def _on(first, name, stream):
     if not first.is_cuda:
         raise ValueError("%s must live on the GPU" % name)
     dev = first.get_device()
-    if dev != torch.cuda.current_device():
+    if dev != _current_gpu():
         raise ValueError("%s lives on cuda:%d, which is not the current GPU" % (name, dev))
     if stream is None:
         return dev, _raw_stream(dev) if _raw_stream else torch.cuda.current_stream().cuda_stream
@@ -628,8 +629,8 @@ def _at(t, dtype, shape, dev, name):
 
 
 def _sizes(T, B, I, V, dtype) -> Tokens:
-    if max(T, B, I, V) >= 2**31 or min(T, B, I, V) < -2**31:
-        raise ValueError("sizes %s must fit 32 bits" % ((T, B, I, V),))
+    if (T | B | I | V) >> 31:
+        raise ValueError("sizes %s must be whole numbers of 31 bits" % ((T, B, I, V),))
     return Tokens(T, B, I, V, _dt(dtype))
 
 
