@@ -518,30 +518,33 @@ constexpr long FEW_SIZE = 1L << 22;
 
 template <int FEW>
 constexpr size_t few_lds(int N) {
-    return (size_t)N * ((FEW + 1) * sizeof(float) + 2 * sizeof(uint16_t));
+    return (size_t)N * ((FEW + 1) * sizeof(float) + sizeof(int32_t) + 2 * sizeof(uint16_t));
 }
 
 template <int FEW>
 __global__ __launch_bounds__(FEW_NT) void few_kernel(EmbedGradArgs a, Sorted q, int N, bool aligned) {
     constexpr int FEW_PITCH = FEW + 1;
-    extern __shared__ float tile[];                             // [N][FEW_PITCH]
-    uint16_t *order = (uint16_t *)(tile + (long)N * FEW_PITCH); // [N] the sorted rows' positions
-    uint16_t *length = order + N;                               // [N] of the run that begins at a row, else 0
-    const int M = q.start[a.V];
-    for (int r = threadIdx.x; r < M; r += FEW_NT) {
-        const int v = q.key[r];
-        order[r] = (uint16_t)q.order[r];
-        length[r] = (uint16_t)(q.start[v] == r ? q.start[v + 1] - r : 0);
-    }
-    const int i0 = blockIdx.x * FEW, ni = min(FEW, a.I - i0), len = ni * a.B;
+    extern __shared__ float tile[];                         // [N][FEW_PITCH]
+    int32_t *key = (int32_t *)(tile + (long)N * FEW_PITCH); // [N] the sorted rows' tokens
+    uint16_t *order = (uint16_t *)(key + N);                // [N] and positions
+    uint16_t *length = order + N;                           // [N] of the run that begins at a row, else 0
+    // an XCD's work-groups (every eighth) take neighbouring features: rows are
+    // written in pieces of 16 or 32 bytes, and only one L2 can join them to lines
+    const int each = gridDim.x / 8, i0 = ((int)blockIdx.x % 8 * each + (int)blockIdx.x / 8) * FEW;
+    if (i0 >= a.I)
+        return;
+    const int ni = min(FEW, a.I - i0), len = ni * a.B;
     // groups of four elements that cover a step's ni * B, which lie in one piece
     const int per = len / 4 + 2;
-    for (long n = threadIdx.x; n < (long)a.T * per; n += FEW_NT) {
-        const int t = (int)(n / per), j = (int)(n - (long)t * per);
-        const long lo = ((long)t * a.I + i0) * a.B, hi = lo + len, e = lo / 4 * 4 + (long)j * 4;
-        if (e >= hi)
-            continue;
-        float f[4];
+    const long groups = (long)a.T * per;
+    long lo = 0, hi = 0, e = 0;
+    int t = 0;
+    float f[4];
+    auto fetch = [&](long n) {
+        t = (int)(n / per);
+        lo = ((long)t * a.I + i0) * a.B;
+        hi = lo + len;
+        e = lo / 4 * 4 + (n - (long)t * per) * 4;
         if (aligned && e >= lo && e + 4 <= hi) {
             vec<float, 4>::load(a.dX + e, f);
         } else {
@@ -549,18 +552,36 @@ __global__ __launch_bounds__(FEW_NT) void few_kernel(EmbedGradArgs a, Sorted q, 
             for (int k = 0; k < 4; ++k)
                 f[k] = e + k >= lo && e + k < hi ? a.dX[e + k] : 0.f;
         }
-        drop_any<4>(a.drop, e, f);
-        const int r = (int)(e - lo);
-        int i = r < 0 ? 0 : r / a.B, b = r - i * a.B;
+    };
+    // a thread's first group is on its way while the tokens are read
+    long n = threadIdx.x;
+    if (n < groups)
+        fetch(n);
+    const int M = q.start[a.V];
+    for (int r = threadIdx.x; r < M; r += FEW_NT) {
+        const int v = q.key[r];
+        key[r] = v;
+        order[r] = (uint16_t)q.order[r];
+        length[r] = (uint16_t)(q.start[v] == r ? q.start[v + 1] - r : 0);
+    }
+    while (n < groups) {
+        if (e < hi) {
+            drop_any<4>(a.drop, e, f);
+            const int r = (int)(e - lo);
+            int i = r < 0 ? 0 : r / a.B, b = r - i * a.B;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (e + k >= lo && e + k < hi)
-                tile[(t * a.B + b) * FEW_PITCH + i] = f[k];
-            if (++b == a.B) {
-                b = 0;
-                ++i;
+            for (int k = 0; k < 4; ++k) {
+                if (e + k >= lo && e + k < hi)
+                    tile[(t * a.B + b) * FEW_PITCH + i] = f[k];
+                if (++b == a.B) {
+                    b = 0;
+                    ++i;
+                }
             }
         }
+        n += FEW_NT;
+        if (n < groups)
+            fetch(n);
     }
     __syncthreads();
     const int i = threadIdx.x % FEW;
@@ -570,7 +591,6 @@ __global__ __launch_bounds__(FEW_NT) void few_kernel(EmbedGradArgs a, Sorted q, 
         const int n = length[r];
         if (n == 0)
             continue;
-        const int v = q.key[r];
         float sum = 0.f;
         int k = 0;
         for (; k + 8 <= n; k += 8) {
@@ -584,7 +604,7 @@ __global__ __launch_bounds__(FEW_NT) void few_kernel(EmbedGradArgs a, Sorted q, 
         }
         for (; k < n; ++k)
             sum += tile[order[r + k] * FEW_PITCH + i];
-        put(a, a.dE + (long)v * a.I + i0 + i, sum);
+        put(a, a.dE + (long)key[r] * a.I + i0 + i, sum);
     }
 }
 
@@ -689,9 +709,9 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
     const bool from = (uintptr_t)a.dX % 16 == 0;
     if (N <= FEW_MOST && (long)N * a.I <= FEW_SIZE) {
         if (a.I <= 4 * FEW_CUS)
-            hipLaunchKernelGGL(few_kernel<4>, dim3((unsigned)ceil_div(a.I, 4)), dim3(FEW_NT), few_lds<4>(N), s, a, q, N, from);
+            hipLaunchKernelGGL(few_kernel<4>, dim3((unsigned)ceil_div(a.I, 32) * 8), dim3(FEW_NT), few_lds<4>(N), s, a, q, N, from);
         else
-            hipLaunchKernelGGL(few_kernel<8>, dim3((unsigned)ceil_div(a.I, 8)), dim3(FEW_NT), few_lds<8>(N), s, a, q, N, from);
+            hipLaunchKernelGGL(few_kernel<8>, dim3((unsigned)ceil_div(a.I, 64) * 8), dim3(FEW_NT), few_lds<8>(N), s, a, q, N, from);
         return hipGetLastError();
     }
     const Tiling g = tiling_of(a.T, a.B, a.I);
