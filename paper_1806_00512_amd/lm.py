@@ -1,0 +1,219 @@
+"""A recurrent language model on the package's kernels: token ids in, loss and
+updated weights out.
+
+  embedding lookup (scaled, with dropout), a stack of LSTM layers with dropout
+  between them and on top, a product with the vocabulary's rows, cross entropy
+  (or the clipped policy loss), and all of it backward, the LSTM layers with
+  the structurally sparsified backward pass in the sparse steps of a
+  dense-after-sparse schedule (section 5).
+
+Every dropout of a step has its own stretch of the counter-based generator, so
+the backward pass asks for the same mask again and none is stored.  The
+vocabulary product is a plain matrix product of one step at a time (torch); the
+rest are liblstmss calls on buffers allocated once.  `python -m
+paper_1806_00512_amd.lm` trains a small model on synthetic sequences.
+"""
+from __future__ import annotations
+
+import math
+from dataclasses import dataclass
+
+import torch
+
+from . import lstmss as L
+
+
+@dataclass
+class LanguageConfig:
+    vocabulary: int
+    features: int                  # of the embedding
+    hidden: int
+    layers: int
+    batch: int
+    steps: int
+    dtype: torch.dtype = torch.float32
+    lr: float = 0.5
+    dropout: float = 0.5
+    seed: int = 1
+    sparsity: float = 0.5
+    P: int = 4
+    R: int = 8
+
+    def layer_input(self, l: int) -> int:
+        return self.features if l == 0 else self.hidden
+
+
+class LanguageModel:
+    """Weights E [V][I], Ws[l] [4H][I_l + H], bs[l] [4H] (fp32), Wv [V][H]; all but the
+    biases in the storage type.  step() and policy_step() train them in place."""
+
+    def __init__(self, cfg: LanguageConfig, E, Ws, bs, Wv, device="cuda:0"):
+        L.load()
+        self.cfg, self.E, self.Ws, self.bs, self.Wv = cfg, E, list(Ws), list(bs), Wv
+        dev, dt, f32 = torch.device(device), cfg.dtype, torch.float32
+        T, B, H, V, I = cfg.steps, cfg.batch, cfg.hidden, cfg.vocabulary, cfg.features
+        if tuple(E.shape) != (V, I) or tuple(Wv.shape) != (V, H) or E.dtype != dt or Wv.dtype != dt:
+            raise ValueError("E must be [%d][%d] and Wv [%d][%d], both %s" % (V, I, V, H, dt))
+        self.scale = math.sqrt(I)
+        self.drawn = 0             # mask elements that earlier steps took
+        e = dict(device=dev)
+        self.inputs, self.houts, self.caches, self.fws, self.outs = [], [], [], [], []
+        ws = 0
+        for l in range(cfg.layers):
+            n = cfg.layer_input(l)
+            if tuple(self.Ws[l].shape) != (4 * H, n + H) or self.Ws[l].dtype != dt:
+                raise ValueError("W[%d] must be [%d][%d] %s" % (l, 4 * H, n + H, dt))
+            d = L.dims(T, B, n, H, dt)
+            self.inputs.append(torch.empty((T, n, B), dtype=dt, **e))
+            self.houts.append(torch.empty((T, H, B), dtype=dt, **e))
+            self.caches.append(torch.empty(L.cache_bytes(d), dtype=torch.uint8, **e))
+            self.fws.append(torch.empty(L.fwd_workspace_bytes(d), dtype=torch.uint8, **e))
+            self.outs.append({"dX": torch.empty((T, n, B), dtype=f32, **e)})
+            s = L.structure(cfg.P, cfg.R)
+            ws = max(ws, L.workspace_bytes(d, 0.0), L.workspace_bytes(d, cfg.sparsity, s))
+        self.ws = torch.empty(ws, dtype=torch.uint8, **e)
+        self.top = torch.empty((T, H, B), dtype=dt, **e)
+        self.logits = torch.empty((T, V, B), dtype=dt, **e)
+        self.loss_out = {"loss": torch.empty(1, dtype=f32, **e), "logp": torch.empty((T, B), dtype=f32, **e),
+                         "dlogits": self.logits}
+        self.loss_ws = torch.empty(L.loss_workspace_bytes(T, B, V, dt), dtype=torch.uint8, **e)
+        self.dH = torch.empty((T, H, B), dtype=f32, **e)
+        self.dWv = torch.empty((V, H), dtype=f32, **e)
+        self.dE = torch.empty((V, I), dtype=f32, **e)
+        self.dE_ws = torch.empty(L.embed_grad_workspace_bytes(T, B, I, V), dtype=torch.uint8, **e)
+
+    def _drops(self, training: bool):
+        """A dropout for the embedding and one for every layer's output, or Nones; the
+        step's share of the generator is taken whether it is used or not."""
+        cfg, out = self.cfg, []
+        for l in range(cfg.layers + 1):
+            n = cfg.steps * cfg.batch * (cfg.features if l == 0 else cfg.hidden)
+            out.append(L.drop(cfg.dropout, cfg.seed, self.drawn) if training and cfg.dropout > 0 else None)
+            self.drawn += -(-n // 8) * 8
+        return out
+
+    def forward(self, tokens, drops):
+        """Logits [T][V][B] of tokens [T][B] (int32)."""
+        L.embed(tokens, self.E, scale=self.scale, drop=drops[0], out=self.inputs[0])
+        for l in range(self.cfg.layers):
+            L.fwd_cache(self.inputs[l], self.Ws[l], self.bs[l], h_out=self.houts[l], cache=self.caches[l],
+                        ws=self.fws[l])
+            nxt = self.inputs[l + 1] if l + 1 < self.cfg.layers else self.top
+            if drops[l + 1] is not None:
+                L.dropout(self.houts[l], drops[l + 1], out=nxt)
+            else:
+                nxt.copy_(self.houts[l])
+        for t in range(self.cfg.steps):
+            torch.mm(self.Wv, self.top[t], out=self.logits[t])
+        return self.logits
+
+    def backward(self, tokens, drops, sparse: bool):
+        """Gradients of everything from dL/dlogits, which stands in the logits' place."""
+        cfg, d = self.cfg, self.logits
+        self.dWv.zero_()
+        for t in range(cfg.steps):
+            self.dH[t] = torch.mm(self.Wv.t(), d[t])
+            self.dWv += torch.mm(d[t], self.top[t].t())
+        up = self.dH
+        for l in range(cfg.layers - 1, -1, -1):
+            if drops[l + 1] is not None:
+                L.dropout(up, drops[l + 1], out=up)
+            call = dict(out=self.outs[l], ws=self.ws)
+            self.outs[l] = L.bwd_structsparse(self.inputs[l], self.Ws[l], self.caches[l], up, sparsity=cfg.sparsity,
+                                              P=cfg.P, R=cfg.R, want_idx=False, **call) if sparse else \
+                L.bwd_dense(self.inputs[l], self.Ws[l], self.caches[l], up, **call)
+            up = self.outs[l]["dX"]
+        L.embed_grad(tokens, up, cfg.vocabulary, scale=self.scale, drop=drops[0], dE=self.dE, ws=self.dE_ws)
+
+    def update(self):
+        """SGD with a fixed learning rate."""
+        lr = self.cfg.lr
+        for l in range(self.cfg.layers):
+            L.sgd_update(self.Ws[l], self.bs[l], self.outs[l]["dW"], self.outs[l]["db"], lr, self.cfg.layer_input(l))
+        self.E.copy_(self.E.float().sub_(self.dE, alpha=lr))
+        self.Wv.copy_(self.Wv.float().sub_(self.dWv, alpha=lr))
+
+    def _loss_scale(self, targets):
+        return 1.0 / (self.cfg.steps * self.cfg.batch)
+
+    def step(self, tokens, targets, sparse: bool = False, update: bool = True):
+        """One training step on targets [T][B] (int32, -1: none); returns the loss [1], the mean
+        over T * B of the targets' -logp."""
+        drops = self._drops(True)
+        self.forward(tokens, drops)
+        L.xent(self.logits, targets, scale=self._loss_scale(targets), out=self.loss_out, ws=self.loss_ws)
+        self.backward(tokens, drops, sparse)
+        if update:
+            self.update()
+        return self.loss_out["loss"]
+
+    def score(self, tokens, targets):
+        """The targets' log probabilities [T][B] without dropout (a new tensor)."""
+        logits = self.forward(tokens, [None] * (self.cfg.layers + 1))
+        return L.token_logp(logits, targets, ws=self.loss_ws)
+
+    def policy_step(self, tokens, targets, old, ref, adv, clip_low=0.2, clip_high=0.2, kl=0.0,
+                    sparse: bool = False, update: bool = True):
+        """One step of the clipped policy loss: old and ref (may be None) are logp as score()
+        gives them, adv the tokens' advantages, all [T][B]."""
+        drops = self._drops(False)
+        self.forward(tokens, drops)
+        L.policy_loss(self.logits, targets, old, ref, adv, clip_low=clip_low, clip_high=clip_high, kl=kl,
+                      scale=self._loss_scale(targets), out=self.loss_out, ws=self.loss_ws)
+        self.backward(tokens, drops, sparse)
+        if update:
+            self.update()
+        return self.loss_out["loss"]
+
+
+def make_weights(cfg: LanguageConfig, device="cuda:0"):
+    """Uniform weights of 0.1, zero biases, from cfg.seed."""
+    g = torch.Generator().manual_seed(cfg.seed)
+
+    def uniform(*shape):
+        return ((torch.rand(shape, generator=g) - 0.5) * 0.2).to(device=device, dtype=cfg.dtype)
+
+    H = cfg.hidden
+    return (uniform(cfg.vocabulary, cfg.features),
+            [uniform(4 * H, cfg.layer_input(l) + H) for l in range(cfg.layers)],
+            [torch.zeros(4 * H, device=device) for _ in range(cfg.layers)],
+            uniform(cfg.vocabulary, H))
+
+
+def synthetic_batch(cfg: LanguageConfig, seed: int, device="cuda:0"):
+    """Tokens and next-token targets of sequences in which a token decides the next (5 times it
+    and 3 more, modulo the vocabulary), half of them padded at the end."""
+    g = torch.Generator().manual_seed(seed)
+    T, B, V = cfg.steps, cfg.batch, cfg.vocabulary
+    rows = [torch.randint(0, V, (B,), generator=g)]
+    for _ in range(T):
+        rows.append((5 * rows[-1] + 3) % V)
+    s = torch.stack(rows)
+    length = torch.where(torch.rand(B, generator=g) < 0.5, T, T - T // 4)
+    s = torch.where(torch.arange(T + 1)[:, None] <= length[None, :], s, -1).to(torch.int32)
+    return s[:-1].contiguous().to(device), s[1:].contiguous().to(device)
+
+
+def main(steps: int = 60):
+    from .train import dense_after_sparse
+    cfg = LanguageConfig(vocabulary=200, features=64, hidden=128, layers=2, batch=32, steps=20, lr=4.0,
+                         dropout=0.1)
+    model = LanguageModel(cfg, *make_weights(cfg))
+    losses = []
+    for k, sparse in enumerate(dense_after_sparse(steps)):
+        losses.append(float(model.step(*synthetic_batch(cfg, k), sparse=sparse)))
+        if k % 10 == 0 or k == steps - 1:
+            print("step %d (%s) loss %.4f" % (k, "sparse" if sparse else "dense", losses[-1]), flush=True)
+    tokens, targets = synthetic_batch(cfg, 1000)
+    before = model.score(tokens, targets)
+    adv = torch.where(torch.arange(cfg.batch, device=tokens.device) % 2 == 0, 1.0, -1.0).expand(cfg.steps, -1)
+    for _ in range(3):
+        model.policy_step(tokens, targets, before, before, adv.contiguous(), kl=0.05)
+    moved = (model.score(tokens, targets) - before).sum(0)
+    print("policy update: logp of favoured sequences %+.3f, of the others %+.3f" %
+          (float(moved[::2].mean()), float(moved[1::2].mean())), flush=True)
+    return losses, moved
+
+
+if __name__ == "__main__":
+    main()

@@ -420,6 +420,79 @@ def test_loss_past_32_bits(L):
         assert torch.allclose(x[t, :, b].double().cpu(), d, rtol=2.0**-7, atol=0)
 
 
+# ------------------------------------------------------------ large tensors
+
+@pytest.mark.parametrize("dtype,n,period", [("f32", 9000000, 0), ("bf16", 17000003, 0), ("f32", 8500001, 4096),
+                                            ("bf16", 17000000, 1000003)])
+def test_dropout_of_large_tensors(L, dtype, n, period):
+    """32 MB and more are written another way."""
+    x = torch.randn(n, device=DEV).to(TYPES[dtype])
+    y = L.dropout(x, L.drop(0.3, 17, 8, period))
+    k = up(O.keep(n, 0.3, 17, 8, period), torch.bool)
+    scale = torch.tensor(O.keep_scale(0.3), dtype=torch.float32, device=DEV)
+    assert torch.equal(y, torch.where(k, x.float() * scale, torch.zeros((), device=DEV)).to(TYPES[dtype]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,B,I,p", [(40, 128, 2048, 0.2), (40, 128, 2048, 0.0), (45, 100, 2047, 0.2),
+                                     (9000, 1, 2048, 0.0), (1300, 13, 1030, 0.2)])
+def test_embed_of_large_tensors(L, dtype, T, B, I, p):
+    rng = np.random.default_rng(T)
+    tok = up(tokens_of(rng, T, B, 500, "some"), torch.int32)
+    E = torch.randn((500, I), device=DEV).to(TYPES[dtype])
+    x = L.embed(tok, E, scale=0.7, drop=L.drop(p, 3) if p else None)
+    ok = (tok >= 0) & (tok < 500)
+    rows = E[torch.where(ok, tok, 0).long()].float() * torch.tensor(0.7, device=DEV)
+    ref = torch.where(ok[..., None], rows, torch.zeros((), device=DEV)).permute(0, 2, 1)
+    if p:
+        k = up(O.keep(x.numel(), p, 3).reshape(x.shape), torch.bool)
+        ref = torch.where(k, ref * torch.tensor(O.keep_scale(p), dtype=torch.float32, device=DEV), torch.zeros((), device=DEV))
+    assert torch.equal(x, ref.to(TYPES[dtype]))
+
+
+@pytest.mark.parametrize("T,B,I,V,p", [(50, 128, 2048, 4000, 0.0), (50, 128, 2048, 4000, 0.3), (60, 64, 1500, 900, 0.0),
+                                       (16, 96, 1100, 500, 0.2), (1, 1900, 2100, 300, 0.0), (70, 30, 1020, 40, 0.0)])
+def test_embed_grad_of_large_tensors(L, T, B, I, V, p):
+    rng = np.random.default_rng(I)
+    tok = up(tokens_of(rng, T, B, V, "zipf"), torch.int32)
+    g = torch.randn((T, I, B), device=DEV)
+    dE = L.embed_grad(tok, g, V, scale=1.5, drop=L.drop(p, 2) if p else None)
+    d = g.double()
+    if p:
+        d = d * up(O.keep(g.numel(), p, 2).reshape(g.shape), torch.float64) * O.keep_scale(p)
+    rows = d.permute(0, 2, 1).reshape(T * B, I) * 1.5
+    at = tok.reshape(-1).long()
+    ref = torch.zeros((V, I), dtype=torch.float64, device=DEV).index_add_(0, at, rows)
+    size = torch.zeros((V, I), dtype=torch.float64, device=DEV).index_add_(0, at, rows.abs())
+    count = torch.bincount(at, minlength=V).double()
+    assert ((dE.double() - ref).abs() <= (count[:, None] + 3) * U * size + 1e-13 * size).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,B", [(2, 20000, 250), (3, 9999, 333), (2, 30000, 640), (4, 40000, 500), (1, 30011, 2100),
+                                   (31, 32001, 128)])
+def test_xent_of_large_tensors(L, dtype, T, V, B):
+    """From 32 MB on the gradient is written another way, from 224 MB on part of the logits is
+    read another way: against the same formula in fp64, step by step."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(V)
+    x = (torch.randn((T, V, B), generator=g, device=DEV) * 3).to(TYPES[dtype])
+    y = torch.randint(-1, V, (T, B), generator=g, device=DEV, dtype=torch.int32)
+    out = L.xent(x, y, scale=0.5)
+    for t in range(T):
+        lsm = torch.log_softmax(x[t].double(), 0)
+        on = (y[t] >= 0).double()
+        at = y[t].clamp(min=0).long()
+        lp = lsm.gather(0, at[None])[0] * on
+        tol = U * (16 * np.sqrt(V) + 16 + 2 * lp.abs())
+        assert ((out["logp"][t].double() - lp).abs() <= tol).all()
+        p = lsm.exp()
+        d = 0.5 * on * p
+        d[at, torch.arange(B, device=DEV)] -= 0.5 * on
+        lim = 0.5 * on * p * (tol + (3 * lsm.abs() + 16) * U) + 2 * U * 0.5 + d.abs() * (2.0**-8 if dtype == "bf16" else 2 * U) + 2.0**-133
+        assert ((out["dlogits"][t].double() - d).abs() <= lim).all()
+
+
 # ------------------------------------------------------------ calls
 
 def test_long_rows_as_one_step(L):
