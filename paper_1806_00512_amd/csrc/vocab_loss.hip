@@ -41,6 +41,19 @@ __device__ __forceinline__ Stat stat_join(Stat a, Stat b) {
     return {m, a.s * __expf(a.m - m) + b.s * __expf(b.m - m)};
 }
 
+// n of them, `step` apart: the largest reference first, so that no exponential
+// waits for another.
+__device__ __forceinline__ Stat stat_join(const Stat *q, int n, int step) {
+    Stat a = {-FLT_MAX, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < n; ++i)
+        a.m = fmaxf(a.m, q[i * step].m);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i)
+        a.s += q[i * step].s * __expf(q[i * step].m - a.m);
+    return a;
+}
+
 // U rows of VEC columns into the columns' running (m, s).  The reference
 // moves only when some value is GROW above it (the sums then rescale), so the
 // usual group costs one exponential for each element and none besides, and
@@ -98,10 +111,10 @@ struct Piece {
     long lo, hi;
 };
 
-__device__ __forceinline__ Piece piece_of(const Cut &g, long block) {
+__device__ __forceinline__ Piece piece_of(const Cut &g, uint32_t block) {
     Piece p;
-    p.t = (int)(block / g.chunks);
-    p.c = (int)(block - (long)p.t * g.chunks);
+    p.t = (int)(block / (uint32_t)g.chunks);
+    p.c = (int)(block - (uint32_t)p.t * g.chunks);
     p.v0 = p.c * g.rows;
     p.v1 = min(g.V, p.v0 + g.rows);
     const long s0 = (long)p.t * g.V * g.B + g.mis;
@@ -110,10 +123,11 @@ __device__ __forceinline__ Piece piece_of(const Cut &g, long block) {
     return p;
 }
 
-// The column of element `at` (counted as in Piece, not before lo - VEC).
+// The column of element `at` (counted as in Piece, after lo - VEC and at most a
+// work-group's vectors from there).
 __device__ __forceinline__ int column_of(const Cut &g, const Piece &p, long at) {
-    const long r = at - p.lo;
-    return (int)((r + (long)g.B * 16) % g.B);
+    const int r = (int)(at - p.lo);
+    return (uint32_t)(r + g.B * 16) % (uint32_t)g.B;
 }
 
 // Whole vectors of the logits, past the caches or not.
@@ -186,13 +200,8 @@ __global__ __launch_bounds__(NT) void stat_flat_kernel(Cut g, const TS *logits, 
         part[q0 + h * g.B] = a;
     }
     __syncthreads();
-    for (int b = j; b < g.B; b += blockDim.x) {
-        const int q0 = (b + g.B - c0) % g.B;
-        Stat a = part[q0];
-        for (int h = 1; h < helpers; ++h)
-            a = stat_join(a, part[q0 + h * g.B]);
-        stat[((long)p.t * g.chunks + p.c) * g.B + b] = a;
-    }
+    for (int b = j; b < g.B; b += blockDim.x)
+        stat[((long)p.t * g.chunks + p.c) * g.B + b] = stat_join(part + (b + g.B - c0) % g.B, helpers, g.B);
 }
 
 template <typename TS, int VEC>
@@ -230,12 +239,8 @@ __global__ __launch_bounds__(NT) void stat_wide_kernel(Cut g, const TS *logits, 
     __syncthreads();
     if (row == 0 && b < g.B)
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-            Stat a = part[k * 64 + lane];
-            for (int r = 1; r < 4; ++r)
-                a = stat_join(a, part[(r * VEC + k) * 64 + lane]);
-            stat[((long)p.t * g.chunks + p.c) * g.B + b + k] = a;
-        }
+        for (int k = 0; k < VEC; ++k)
+            stat[((long)p.t * g.chunks + p.c) * g.B + b + k] = stat_join(part + k * 64 + lane, 4, VEC * 64);
 }
 
 // What the gradient kernel needs of a token: dL/dx_v = p * exp(min(x_v - lse, 1)),
@@ -281,9 +286,7 @@ __global__ __launch_bounds__(NT) void token_kernel(LossArgs a, int chunks, const
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 r[u] = c + u * SUBS < chunks ? stat[((long)t * chunks + c + u * SUBS) * a.B + b] : Stat{-FLT_MAX, 0.f};
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                q = stat_join(q, r[u]);
+            q = stat_join(q, stat_join(r, U, 1));
         }
 #pragma unroll
     for (int m = TOKENS; m < 64; m <<= 1)
@@ -293,8 +296,7 @@ __global__ __launch_bounds__(NT) void token_kernel(LossArgs a, int chunks, const
     __syncthreads();
     if (threadIdx.x >= TOKENS)
         return;
-    for (int r = 1; r < NT / 64; ++r)
-        q = stat_join(q, join[r][j]);
+    q = stat_join(&join[0][j], NT / 64, TOKENS);
     double term = 0.0;
     if (n < N) {
         double lp = 0.0, g = 0.0;
@@ -493,13 +495,20 @@ __global__ __launch_bounds__(NT) void grad_wide_kernel(Cut g, const TS *logits, 
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// A work-group's share of a step: PIECE bytes of logits, in the first kernel
-// more where that makes over GROUPS work-groups (each leaves (m, s) of every
-// column), and whole multiples of PIECE where a number of rows comes to that.
+// A work-group's share of a step: PIECE bytes of logits or more, and whole
+// multiples of PIECE where a number of rows comes to that.  Each of the first
+// kernel's leaves (m, s) of every column, which costs it and the token kernel
+// time: 512 of them, as many more as get 48 KB each, and 2048 at most (us of the
+// whole loss with 2048, 1024 and 512 of them: 35 x 10000 x 20 fp32 23.0, 22.7, 22.2;
+// 35 x 10000 x 64 bf16 33.2, 32.0, 32.2; 50 x 32000 x 128 bf16 200, 208, 203).
 // The gradient's work-groups leave nothing, so finer ones only end more evenly.
 // 50 x 32000 x 128 bf16, loss and gradient, us by the gradient's piece: 32 KB 205,
 // 16 KB 200, 8 KB 238, 4 KB 310; of about 25 KB, not on such boundaries, 223.
-constexpr long PIECE = 16384, GROUPS = 2048, GRAD_GROUPS = 1L << 22;
+constexpr long PIECE = 16384, SHARE = 3 * PIECE, GRAD_GROUPS = 1L << 22;
+
+long stat_groups(int T, int B, int V, int es) {
+    return std::max(512L, std::min(2048L, (long)T * V * B * es / SHARE));
+}
 
 // What of the logits the first kernel leaves in the last-level cache (256 MB)
 // for the gradient: the last of them; what comes before is read past it, which
@@ -595,11 +604,12 @@ template <typename TS>
 hipError_t dispatch(const LossArgs &a, hipStream_t s) {
     constexpr int VEC = vec_of<TS>(), ES = st<TS>::bytes;
     const int mis = (int)((uintptr_t)a.logits / ES % VEC);
+    const long groups = stat_groups(a.T, a.B, a.V, ES);
     const bool alike = !a.dlogits || (int)((uintptr_t)a.dlogits / ES % VEC) == mis;
-    Cut g = cut_of(a.T, a.B, a.V, ES, VEC, mis, GROUPS);
+    Cut g = cut_of(a.T, a.B, a.V, ES, VEC, mis, groups);
     if (alike && (g.lanes || (mis == 0 && a.B % VEC == 0)))
         return run<TS, VEC>(a, g, layout(a.ws, a.T, a.B, g.chunks), s);
-    g = cut_of(a.T, a.B, a.V, ES, 1, 0, GROUPS);
+    g = cut_of(a.T, a.B, a.V, ES, 1, 0, groups);
     return run<TS, 1>(a, g, layout(a.ws, a.T, a.B, g.chunks), s);
 }
 
@@ -608,7 +618,8 @@ hipError_t dispatch(const LossArgs &a, hipStream_t s) {
 // For either cut: where the tensors start is not known here.
 size_t loss_ws(int T, int B, int V, bool bf16) {
     const int es = bf16 ? 2 : 4;
-    const int a = cut_of(T, B, V, es, 16 / es, 0, GROUPS).chunks, b = cut_of(T, B, V, es, 1, 0, GROUPS).chunks;
+    const long groups = stat_groups(T, B, V, es);
+    const int a = cut_of(T, B, V, es, 16 / es, 0, groups).chunks, b = cut_of(T, B, V, es, 1, 0, groups).chunks;
     return layout(nullptr, T, B, (size_t)std::max(a, b)).bytes;
 }
 
