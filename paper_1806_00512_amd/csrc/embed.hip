@@ -97,9 +97,8 @@ __device__ __forceinline__ void for_whole_groups(const Tiling &g, const Tile &a,
 }
 
 // A tile's elements, scaled and with dropout, from LDS to x.
-template <typename TS>
-__device__ __forceinline__ void write_tile(const EmbedArgs &a, const Tiling &g, const Tile &w, const float *tile, TS *x,
-                                           bool aligned, bool past) {
+template <bool PAST, typename TS>
+__device__ __forceinline__ void write_tile(const EmbedArgs &a, const Tiling &g, const Tile &w, const float *tile, TS *x) {
     constexpr int VEC = vec_of<TS>();
     for_groups<VEC>(g, w, [&](long e, long lo, long hi, int i, int b, bool whole) {
         float f[VEC];
@@ -118,22 +117,20 @@ __device__ __forceinline__ void write_tile(const EmbedArgs &a, const Tiling &g, 
             }
         }
         drop_any<VEC>(a.drop, e, f);
-        if (aligned && e >= lo && e + VEC <= hi)
-            return store16(x + e, f, past);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k)
-            if (e + k >= lo && e + k < hi)
-                st<TS>::store(x, e + k, f[k]);
+        if (e >= lo && e + VEC <= hi)
+            store16<PAST>(x + e, f);
+        else
+            store_part(x + e, (int)max(lo - e, 0L), (int)min(hi - e, (long)VEC), f);
     });
 }
 
 // A work-group's columns and `run` feature tiles one after the other: the next
 // tile's rows are on their way while this one is turned over and written.
-// WHOLE: B is a multiple of 64 and x 16-byte aligned, the mask repeats after a
-// multiple of 8 if at all; DROP: with dropout (only told apart there).
-template <typename TS, int LV, bool WHOLE, bool DROP>
-__global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int run, bool aligned, bool past) {
-    constexpr int PER = TILE / LV, LOADS = TILE * PER / NT;
+// WHOLE: B is a multiple of 64, and the mask repeats after a multiple of 8 if
+// at all; DROP: with dropout (only told apart there).  PAST: x is streamed.
+template <typename TS, bool WHOLE, bool DROP, bool PAST>
+__global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int run) {
+    constexpr int LV = vec_of<TS>(), PER = TILE / LV, LOADS = TILE * PER / NT;
     __shared__ float tile[TILE * PITCH];
     const int runs = (g.tiles + run - 1) / run;
     const int part = blockIdx.x % runs;
@@ -152,13 +149,10 @@ __global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int ru
     auto fetch = [&](int i0) {
 #pragma unroll
         for (int k = 0; k < LOADS; ++k) {
-            if (row[k] && i0 + i < g.I) {
-                vec<TS, LV>::load(row[k] + i0 + i, f[k]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < LV; ++j)
-                    f[k][j] = 0.f;
-            }
+            if (row[k] && i0 + i + LV <= g.I)
+                load16(row[k] + i0 + i, f[k]);
+            else
+                load_part(row[k] + i0 + i, 0, row[k] ? g.I - i0 - i : 0, f[k], 0.f);
         }
     };
     fetch(w.i0);
@@ -185,10 +179,10 @@ __global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a, Tiling g, int ru
                     o[k] = tile[(b + k) * PITCH + i] * a.scale;
                 if (DROP)
                     drop_whole<VEC>(a.drop, e, o);
-                store16(x + e, o, past);
+                store16<PAST>(x + e, o);
             });
         } else
-            write_tile(a, g, w, tile, x, aligned, past);
+            write_tile<PAST>(a, g, w, tile, x);
         __syncthreads();
     }
 }
@@ -200,14 +194,13 @@ constexpr int SORT_NT = 1024, SORT_WAVES = SORT_NT / 64, SORT_MOST = 512;
 constexpr long FILL = 16384; // elements that a work-group zeroes
 
 __device__ __forceinline__ void zero_fill(float *p, long i0, long i1) {
-    // whole vectors between the first and the last 16-byte boundary, the rest singly
-    const long v0 = i0 + (4 - (long)((uintptr_t)(p + i0) / 4 % 4)) % 4, v1 = i1 - (long)((uintptr_t)(p + i1) / 4 % 4);
-    for (long i = v0 + threadIdx.x * 4; i < v1; i += SORT_NT * 4)
-        *(f32x4 *)(p + i) = f32x4{0.f, 0.f, 0.f, 0.f};
-    if ((long)threadIdx.x < v0 - i0 && i0 + (long)threadIdx.x < i1)
-        p[i0 + threadIdx.x] = 0.f;
-    if (v1 >= v0 && (long)threadIdx.x < i1 - v1)
-        p[v1 + threadIdx.x] = 0.f;
+    const float zero[4] = {};
+    for (long i = i0 + threadIdx.x * 4; i < i1; i += SORT_NT * 4) {
+        if (i + 4 <= i1)
+            store16(p + i, zero);
+        else
+            store_part(p + i, 0, (int)(i1 - i), zero);
+    }
 }
 
 // Work-group w places the tokens [w R, (w + 1) R): every wave counts its share
@@ -310,16 +303,13 @@ __device__ __forceinline__ void put(const EmbedGradArgs &a, float *p, float sum)
 }
 
 // A tile of dX, with dropout, into LDS.
-__device__ __forceinline__ void turn_in(const EmbedGradArgs &a, const Tiling &g, const Tile &w, float *tile, bool aligned) {
+__device__ __forceinline__ void turn_in(const EmbedGradArgs &a, const Tiling &g, const Tile &w, float *tile) {
     for_groups<4>(g, w, [&](long e, long lo, long hi, int i, int b, bool whole) {
         float f[4];
-        if (aligned && e >= lo && e + 4 <= hi) {
-            vec<float, 4>::load(a.dX + e, f);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                f[k] = e + k >= lo && e + k < hi ? a.dX[e + k] : 0.f;
-        }
+        if (e >= lo && e + 4 <= hi)
+            load16(a.dX + e, f);
+        else
+            load_part(a.dX + e, (int)max(lo - e, 0L), (int)min(hi - e, 4L), f, 0.f);
         drop_any<4>(a.drop, e, f);
         if (whole) {
 #pragma unroll
@@ -343,7 +333,7 @@ __device__ __forceinline__ void turn_in(const EmbedGradArgs &a, const Tiling &g,
 // tiles one after the other, the next tile's elements on their way meanwhile
 // (WHOLE).
 template <bool WHOLE, bool DROP>
-__global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sorted q, float *rows, int run, bool aligned) {
+__global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sorted q, float *rows, int run) {
     constexpr int PER = TILE / 4, LOADS = TILE * PER / NT;
     __shared__ float tile[TILE * PITCH];
     __shared__ float *dest[TILE];
@@ -359,7 +349,7 @@ __global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sor
         for (int k = 0; k < LOADS; ++k) {
             const int i = threadIdx.x / PER + k * (NT / PER);
             if (i0 + i < g.I)
-                load_past(a.dX + lo + i * g.B, f[k]);
+                load16<true>(a.dX + lo + i * g.B, f[k]);
         }
     };
     if (WHOLE)
@@ -393,7 +383,7 @@ __global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sor
                     tile[(b + j) * PITCH + i] = f[k][j];
             }
         } else {
-            turn_in(a, g, w, tile, aligned);
+            turn_in(a, g, w, tile);
         }
         __syncthreads();
         if (WHOLE && n + 1 < last)
@@ -417,9 +407,9 @@ __global__ __launch_bounds__(NT) void turn_kernel(EmbedGradArgs a, Tiling g, Sor
 // of runs of equal tokens.  A run that begins and ends here is finished; what
 // continues from the group before goes to carry[q][0], what begins here and
 // goes on to carry[q][1].
-template <int G, int VEC>
+template <int G>
 __global__ __launch_bounds__(NT) void walk_kernel(EmbedGradArgs a, Sorted q, const float *rows, float *carry, int parts) {
-    constexpr int U = 8;
+    constexpr int U = 8, VEC = 4;
     __shared__ int key[G + 2];
     const int group = blockIdx.x / parts, part = blockIdx.x - group * parts;
     const int M = q.start[a.V];
@@ -433,8 +423,21 @@ __global__ __launch_bounds__(NT) void walk_kernel(EmbedGradArgs a, Sorted q, con
     }
     __syncthreads();
     const int i = (part * NT + threadIdx.x) * VEC;
-    if (i >= a.I)
+    const int ni = min(VEC, a.I - i);
+    if (ni <= 0)
         return;
+    auto load = [&](const float *p, float *f) {
+        if (ni == VEC)
+            load16(p, f);
+        else
+            load_part(p, 0, ni, f, 0.f);
+    };
+    auto store = [&](float *p, const float *f) {
+        if (ni == VEC)
+            store16(p, f);
+        else
+            store_part(p, 0, ni, f);
+    };
     float sum[VEC] = {};
     bool begun = key[0] != key[1]; // the run at hand begins in this group
     for (int k0 = 0; k0 < n; k0 += U) {
@@ -444,7 +447,7 @@ __global__ __launch_bounds__(NT) void walk_kernel(EmbedGradArgs a, Sorted q, con
             const int k = k0 + u;
             // a row whose token stands once is not there
             if (k < n && (key[k] == key[k + 1] || key[k + 1] == key[k + 2]))
-                vec<float, VEC>::load(rows + (r0 + k) * a.I + i, f[u]);
+                load(rows + (r0 + k) * a.I + i, f[u]);
             else
 #pragma unroll
                 for (int j = 0; j < VEC; ++j)
@@ -469,15 +472,14 @@ __global__ __launch_bounds__(NT) void walk_kernel(EmbedGradArgs a, Sorted q, con
                     float *p = a.dE + (long)v * a.I + i;
                     float out[VEC] = {};
                     if (a.accumulate)
-                        vec<float, VEC>::load(p, out);
+                        load(p, out);
 #pragma unroll
                     for (int j = 0; j < VEC; ++j)
                         out[j] = a.accumulate ? out[j] + sum[j] * a.scale : sum[j] * a.scale;
-                    vec<float, VEC>::store(p, out);
+                    store(p, out);
                 }
             } else {
-                float *p = carry + ((long)group * 2 + (begun ? 1 : 0)) * a.I + i;
-                vec<float, VEC>::store(p, sum);
+                store(carry + ((long)group * 2 + (begun ? 1 : 0)) * a.I + i, sum);
             }
 #pragma unroll
             for (int j = 0; j < VEC; ++j)
@@ -522,7 +524,7 @@ constexpr size_t few_lds(int N) {
 }
 
 template <int FEW>
-__global__ __launch_bounds__(FEW_NT) void few_kernel(EmbedGradArgs a, Sorted q, int N, bool aligned) {
+__global__ __launch_bounds__(FEW_NT) void few_kernel(EmbedGradArgs a, Sorted q, int N) {
     constexpr int FEW_PITCH = FEW + 1;
     extern __shared__ float tile[];                         // [N][FEW_PITCH]
     int32_t *key = (int32_t *)(tile + (long)N * FEW_PITCH); // [N] the sorted rows' tokens
@@ -545,13 +547,10 @@ __global__ __launch_bounds__(FEW_NT) void few_kernel(EmbedGradArgs a, Sorted q, 
         lo = ((long)t * a.I + i0) * a.B;
         hi = lo + len;
         e = lo / 4 * 4 + (n - (long)t * per) * 4;
-        if (aligned && e >= lo && e + 4 <= hi) {
-            vec<float, 4>::load(a.dX + e, f);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                f[k] = e + k >= lo && e + k < hi ? a.dX[e + k] : 0.f;
-        }
+        if (e >= lo && e + 4 <= hi)
+            load16(a.dX + e, f);
+        else
+            load_part(a.dX + e, (int)max(lo - e, 0L), (int)min(hi - e, 4L), f, 0.f);
     };
     // a thread's first group is on its way while the tokens are read
     long n = threadIdx.x;
@@ -649,36 +648,28 @@ GradWs layout(void *ws, int N, int I, int V) {
     return w;
 }
 
-template <typename TS>
+template <typename TS, bool PAST>
 hipError_t lookup(const EmbedArgs &a, hipStream_t s) {
-    constexpr int LV = vec_of<TS>();
     const Tiling g = tiling_of(a.T, a.B, a.I);
     // runs of up to four tiles while 2048 work-groups (eight on a CU) are left
     const long steps = (long)g.T * g.chunks;
     const int run = (int)std::max(1L, std::min(4L, steps * g.tiles / 2048));
     const dim3 grid((unsigned)(steps * ceil_div(g.tiles, run)));
-    const bool past = (long)a.T * a.I * a.B * st<TS>::bytes >= STREAM_BYTES;
-    const bool aligned = (uintptr_t)a.x % 16 == 0, rows = (uintptr_t)a.E % 16 == 0 && a.I % LV == 0;
-    if (rows && aligned && a.B % TILE == 0 && a.drop.thr == 0)
-        hipLaunchKernelGGL((embed_kernel<TS, LV, true, false>), grid, dim3(NT), 0, s, a, g, run, aligned, past);
-    else if (rows && aligned && a.B % TILE == 0 && a.drop.period % 8 == 0)
-        hipLaunchKernelGGL((embed_kernel<TS, LV, true, true>), grid, dim3(NT), 0, s, a, g, run, aligned, past);
-    else if (rows)
-        hipLaunchKernelGGL((embed_kernel<TS, LV, false, true>), grid, dim3(NT), 0, s, a, g, run, aligned, past);
+    if (a.B % TILE == 0 && a.drop.thr == 0)
+        hipLaunchKernelGGL((embed_kernel<TS, true, false, PAST>), grid, dim3(NT), 0, s, a, g, run);
+    else if (a.B % TILE == 0 && a.drop.period % 8 == 0)
+        hipLaunchKernelGGL((embed_kernel<TS, true, true, PAST>), grid, dim3(NT), 0, s, a, g, run);
     else
-        hipLaunchKernelGGL((embed_kernel<TS, 1, false, true>), grid, dim3(NT), 0, s, a, g, run, aligned, past);
+        hipLaunchKernelGGL((embed_kernel<TS, false, true, PAST>), grid, dim3(NT), 0, s, a, g, run);
     return hipGetLastError();
 }
 
 template <int G>
-hipError_t walk(const EmbedGradArgs &a, const Sorted &q, const GradWs &w, int N, bool aligned, hipStream_t s) {
+hipError_t walk(const EmbedGradArgs &a, const Sorted &q, const GradWs &w, int N, hipStream_t s) {
     const int groups = (int)ceil_div(N, G);
-    const int parts = (int)ceil_div(a.I, NT * (aligned ? 4 : 1));
+    const int parts = (int)ceil_div(a.I, NT * 4);
     const dim3 grid((unsigned)((long)groups * parts));
-    if (aligned)
-        hipLaunchKernelGGL((walk_kernel<G, 4>), grid, dim3(NT), 0, s, a, q, w.rows, w.carry, parts);
-    else
-        hipLaunchKernelGGL((walk_kernel<G, 1>), grid, dim3(NT), 0, s, a, q, w.rows, w.carry, parts);
+    hipLaunchKernelGGL((walk_kernel<G>), grid, dim3(NT), 0, s, a, q, w.rows, w.carry, parts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || groups < 2)
         return e;
@@ -690,7 +681,9 @@ hipError_t walk(const EmbedGradArgs &a, const Sorted &q, const GradWs &w, int N,
 } // namespace
 
 hipError_t launch_embed(const EmbedArgs &a, bool bf16, hipStream_t s) {
-    return bf16 ? lookup<bf16_t>(a, s) : lookup<float>(a, s);
+    if ((long)a.T * a.I * a.B * (bf16 ? 2 : 4) >= STREAM_BYTES)
+        return bf16 ? lookup<bf16_t, true>(a, s) : lookup<float, true>(a, s);
+    return bf16 ? lookup<bf16_t, false>(a, s) : lookup<float, false>(a, s);
 }
 
 size_t embed_grad_ws(int T, int B, int I, int V) { return layout(nullptr, T * B, I, V).bytes; }
@@ -706,30 +699,28 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    const bool from = (uintptr_t)a.dX % 16 == 0;
     if (N <= FEW_MOST && (long)N * a.I <= FEW_SIZE) {
         if (a.I <= 4 * FEW_CUS)
-            hipLaunchKernelGGL(few_kernel<4>, dim3((unsigned)ceil_div(a.I, 32) * 8), dim3(FEW_NT), few_lds<4>(N), s, a, q, N, from);
+            hipLaunchKernelGGL(few_kernel<4>, dim3((unsigned)ceil_div(a.I, 32) * 8), dim3(FEW_NT), few_lds<4>(N), s, a, q, N);
         else
-            hipLaunchKernelGGL(few_kernel<8>, dim3((unsigned)ceil_div(a.I, 64) * 8), dim3(FEW_NT), few_lds<8>(N), s, a, q, N, from);
+            hipLaunchKernelGGL(few_kernel<8>, dim3((unsigned)ceil_div(a.I, 64) * 8), dim3(FEW_NT), few_lds<8>(N), s, a, q, N);
         return hipGetLastError();
     }
     const Tiling g = tiling_of(a.T, a.B, a.I);
     // runs of up to four tiles while 2048 work-groups (eight on a CU) are left
     const long steps = (long)g.T * g.chunks;
     const int run = (int)std::max(1L, std::min(4L, steps * g.tiles / 2048));
-    const bool aligned = a.I % 4 == 0 && (uintptr_t)a.dE % 16 == 0;
     const dim3 grid((unsigned)(steps * ceil_div(g.tiles, run)));
-    const bool whole = from && a.B % TILE == 0;
+    const bool whole = a.B % TILE == 0;
     if (whole && a.drop.thr == 0)
-        hipLaunchKernelGGL((turn_kernel<true, false>), grid, dim3(NT), 0, s, a, g, q, w.rows, run, from);
+        hipLaunchKernelGGL((turn_kernel<true, false>), grid, dim3(NT), 0, s, a, g, q, w.rows, run);
     else if (whole && a.drop.period % 8 == 0)
-        hipLaunchKernelGGL((turn_kernel<true, true>), grid, dim3(NT), 0, s, a, g, q, w.rows, run, from);
+        hipLaunchKernelGGL((turn_kernel<true, true>), grid, dim3(NT), 0, s, a, g, q, w.rows, run);
     else
-        hipLaunchKernelGGL((turn_kernel<false, true>), grid, dim3(NT), 0, s, a, g, q, w.rows, run, from);
+        hipLaunchKernelGGL((turn_kernel<false, true>), grid, dim3(NT), 0, s, a, g, q, w.rows, run);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
-    return group_of(N) == 16 ? walk<16>(a, q, w, N, aligned, s) : walk<64>(a, q, w, N, aligned, s);
+    return group_of(N) == 16 ? walk<16>(a, q, w, N, s) : walk<64>(a, q, w, N, s);
 }
 
 } // namespace lstmss

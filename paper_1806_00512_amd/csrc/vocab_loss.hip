@@ -16,6 +16,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <numeric>
+#include <type_traits>
 
 #include "common.h"
 #include "language.h"
@@ -100,7 +101,6 @@ struct Cut {
     int rows, chunks;  // rows of a chunk, chunks of a step
     int lanes;         // FLAT: threads at work; WIDE: 0
     int windows;       // WIDE: windows of 64 * VEC columns
-    bool past;         // the gradient is streamed
     unsigned first;    // work-groups below it read the logits past the caches
     int mis;           // elements from the 16-byte boundary before the logits to their start
 };
@@ -130,29 +130,28 @@ __device__ __forceinline__ int column_of(const Cut &g, const Piece &p, long at) 
     return (uint32_t)(r + g.B * 16) % (uint32_t)g.B;
 }
 
-// Whole vectors of the logits, past the caches or not.
-template <typename TS, int VEC>
-__device__ __forceinline__ void load_logits(const TS *x, float *f, bool past) {
-    if constexpr (VEC > 1) {
-        if (past)
-            return load_past(x, f);
-    }
-    vec<TS, VEC>::load(x, f);
+// f with std::true_type or std::false_type.
+template <class F>
+__device__ __forceinline__ void either(bool yes, F &&f) {
+    if (yes)
+        f(std::true_type());
+    else
+        f(std::false_type());
 }
 
 // VEC elements at `at`, those outside [lo, hi) -inf and not touched.
-template <typename TS, int VEC>
+template <typename TS>
 __device__ __forceinline__ void load_edge(const TS *x, long at, long lo, long hi, float *f) {
+    constexpr int VEC = vec_of<TS>();
     if (at >= lo && at + VEC <= hi)
-        return vec<TS, VEC>::load(x + at, f);
-#pragma unroll
-    for (int k = 0; k < VEC; ++k)
-        f[k] = at + k >= lo && at + k < hi ? st<TS>::load(x, at + k) : -INFINITY;
+        load16(x + at, f);
+    else
+        load_part(x + at, (int)max(lo - at, 0L), (int)min(hi - at, (long)VEC), f, -INFINITY);
 }
 
-template <typename TS, int VEC>
+template <typename TS>
 __global__ __launch_bounds__(NT) void stat_flat_kernel(Cut g, const TS *logits, Stat *stat) {
-    constexpr int U = 4;
+    constexpr int U = 4, VEC = vec_of<TS>();
     __shared__ Stat part[NT * VEC];
     const bool past = blockIdx.x < g.first;
     const Piece p = piece_of(g, blockIdx.x);
@@ -169,19 +168,21 @@ __global__ __launch_bounds__(NT) void stat_flat_kernel(Cut g, const TS *logits, 
         }
         long at = first + (long)j * VEC;
         float f[U][VEC];
-        if (VEC > 1 && at < p.lo) {
-            load_edge<TS, VEC>(x, at, p.lo, p.hi, f[0]);
+        if (at < p.lo) {
+            load_edge(x, at, p.lo, p.hi, f[0]);
             stat_add<1, VEC>(f, m, s);
             at += step;
         }
-        for (; at + (U - 1) * step + VEC <= p.hi; at += U * step) {
+        either(past, [&](auto how) {
+            for (; at + (U - 1) * step + VEC <= p.hi; at += U * step) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                load_logits<TS, VEC>(x + at + u * step, f[u], past);
-            stat_add<U, VEC>(f, m, s);
-        }
+                for (int u = 0; u < U; ++u)
+                    load16<how.value>(x + at + u * step, f[u]);
+                stat_add<U, VEC>(f, m, s);
+            }
+        });
         for (; at < p.hi; at += step) {
-            load_edge<TS, VEC>(x, at, p.lo, p.hi, f[0]);
+            load_edge(x, at, p.lo, p.hi, f[0]);
             stat_add<1, VEC>(f, m, s);
         }
 #pragma unroll
@@ -204,32 +205,38 @@ __global__ __launch_bounds__(NT) void stat_flat_kernel(Cut g, const TS *logits, 
         stat[((long)p.t * g.chunks + p.c) * g.B + b] = stat_join(part + (b + g.B - c0) % g.B, helpers, g.B);
 }
 
-template <typename TS, int VEC>
+template <typename TS>
 __global__ __launch_bounds__(NT) void stat_wide_kernel(Cut g, const TS *logits, Stat *stat) {
-    constexpr int U = 4;
+    constexpr int U = 4, VEC = vec_of<TS>();
     __shared__ Stat part[NT * VEC];
     const bool past = blockIdx.x < g.first;
     const Piece p = piece_of(g, blockIdx.x / g.windows);
     const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
-    const long b = ((long)(blockIdx.x % g.windows) * 64 + lane) * VEC;
+    const int b = ((int)(blockIdx.x % g.windows) * 64 + lane) * VEC, nb = min(VEC, g.B - b);
     float m[VEC], s[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
         m[k] = -FLT_MAX;
         s[k] = 0.f;
     }
-    if (b < g.B) {
+    if (nb > 0) {
         const TS *x = logits + (long)p.t * g.V * g.B + b;
         float f[U][VEC];
         int v = p.v0 + row;
-        for (; v + (U - 1) * 4 < p.v1; v += U * 4) {
+        if (nb == VEC)
+            either(past, [&](auto how) {
+                for (; v + (U - 1) * 4 < p.v1; v += U * 4) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                load_logits<TS, VEC>(x + (long)(v + u * 4) * g.B, f[u], past);
-            stat_add<U, VEC>(f, m, s);
-        }
+                    for (int u = 0; u < U; ++u)
+                        load16<how.value>(x + (long)(v + u * 4) * g.B, f[u]);
+                    stat_add<U, VEC>(f, m, s);
+                }
+            });
         for (; v < p.v1; v += 4) {
-            vec<TS, VEC>::load(x + (long)v * g.B, f[0]);
+            if (nb == VEC)
+                load16(x + (long)v * g.B, f[0]);
+            else
+                load_part(x + (long)v * g.B, 0, nb, f[0], -INFINITY);
             stat_add<1, VEC>(f, m, s);
         }
     }
@@ -237,9 +244,8 @@ __global__ __launch_bounds__(NT) void stat_wide_kernel(Cut g, const TS *logits, 
     for (int k = 0; k < VEC; ++k)
         part[(row * VEC + k) * 64 + lane] = {m[k], s[k]};
     __syncthreads();
-    if (row == 0 && b < g.B)
-#pragma unroll
-        for (int k = 0; k < VEC; ++k)
+    if (row == 0)
+        for (int k = 0; k < nb; ++k)
             stat[((long)p.t * g.chunks + p.c) * g.B + b + k] = stat_join(part + k * 64 + lane, 4, VEC * 64);
 }
 
@@ -386,10 +392,11 @@ __device__ __forceinline__ void grad_targets(const Cut &g, const Piece &p, int b
     }
 }
 
-template <typename TS, int VEC>
+// PAST: the gradient is streamed.
+template <typename TS, bool PAST>
 __global__ __launch_bounds__(NT) void grad_flat_kernel(Cut g, const TS *logits, TS *dlogits, const int32_t *targets,
                                                        const Coef *coef, const float *dtarget, LossOut o) {
-    constexpr int U = 4;
+    constexpr int U = 4, VEC = vec_of<TS>();
     if (o.loss && blockIdx.x == 0)
         loss_sum(o);
     const bool past = gridDim.x - 1 - blockIdx.x < g.first;
@@ -410,37 +417,32 @@ __global__ __launch_bounds__(NT) void grad_flat_kernel(Cut g, const TS *logits, 
         }
         float f[U][VEC];
         auto edge = [&] {
-            load_edge<TS, VEC>(x, at, p.lo, p.hi, f[0]);
+            load_edge(x, at, p.lo, p.hi, f[0]);
 #pragma unroll
             for (int k = 0; k < VEC; ++k)
                 f[0][k] = grad_of(f[0][k], c[k]);
-            if (at >= p.lo && at + VEC <= p.hi) {
-                vec<TS, VEC>::store(y + at, f[0]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < VEC; ++k)
-                    if (at + k >= p.lo && at + k < p.hi)
-                        st<TS>::store(y, at + k, f[0][k]);
-            }
+            if (at >= p.lo && at + VEC <= p.hi)
+                store16(y + at, f[0]);
+            else
+                store_part(y + at, (int)max(p.lo - at, 0L), (int)min(p.hi - at, (long)VEC), f[0]);
             at += step;
         };
-        if (VEC > 1 && at < p.lo)
+        if (at < p.lo)
             edge();
-        for (; at + (U - 1) * step + VEC <= p.hi; at += U * step) {
+        either(past, [&](auto how) {
+            for (; at + (U - 1) * step + VEC <= p.hi; at += U * step) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                load_logits<TS, VEC>(x + at + u * step, f[u], past);
+                for (int u = 0; u < U; ++u)
+                    load16<how.value>(x + at + u * step, f[u]);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+                for (int u = 0; u < U; ++u) {
 #pragma unroll
-                for (int k = 0; k < VEC; ++k)
-                    f[u][k] = grad_of(f[u][k], c[k]);
-                if constexpr (VEC > 1)
-                    store16(y + at + u * step, f[u], g.past);
-                else
-                    vec<TS, VEC>::store(y + at + u * step, f[u]);
+                    for (int k = 0; k < VEC; ++k)
+                        f[u][k] = grad_of(f[u][k], c[k]);
+                    store16<PAST>(y + at + u * step, f[u]);
+                }
             }
-        }
+        });
         while (at < p.hi)
             edge();
     }
@@ -448,45 +450,53 @@ __global__ __launch_bounds__(NT) void grad_flat_kernel(Cut g, const TS *logits, 
     grad_targets(g, p, 0, g.B, targets, dtarget, dlogits);
 }
 
-template <typename TS, int VEC>
+// PAST: the gradient is streamed.
+template <typename TS, bool PAST>
 __global__ __launch_bounds__(NT) void grad_wide_kernel(Cut g, const TS *logits, TS *dlogits, const int32_t *targets,
                                                        const Coef *coef, const float *dtarget, LossOut o) {
-    constexpr int U = 4;
+    constexpr int U = 4, VEC = vec_of<TS>();
     if (o.loss && blockIdx.x == 0)
         loss_sum(o);
     const bool past = gridDim.x - 1 - blockIdx.x < g.first;
     const Piece p = piece_of(g, (gridDim.x - 1 - blockIdx.x) / g.windows);
     const int lane = threadIdx.x & 63, row = threadIdx.x >> 6;
-    const int w0 = (int)((gridDim.x - 1 - blockIdx.x) % g.windows) * 64 * VEC, b = w0 + lane * VEC;
-    if (b < g.B) {
+    const int w0 = (int)((gridDim.x - 1 - blockIdx.x) % g.windows) * 64 * VEC, b = w0 + lane * VEC, nb = min(VEC, g.B - b);
+    if (nb > 0) {
         Coef c[VEC];
 #pragma unroll
         for (int k = 0; k < VEC; ++k)
-            c[k] = coef[(long)p.t * g.B + b + k];
+            c[k] = k < nb ? coef[(long)p.t * g.B + b + k] : Coef{0.f, 0.f};
         const long s0 = (long)p.t * g.V * g.B + b;
         float f[U][VEC];
         int v = p.v0 + row;
-        for (; v + (U - 1) * 4 < p.v1; v += U * 4) {
+        if (nb == VEC)
+            either(past, [&](auto how) {
+                for (; v + (U - 1) * 4 < p.v1; v += U * 4) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                load_logits<TS, VEC>(logits + s0 + (long)(v + u * 4) * g.B, f[u], past);
+                    for (int u = 0; u < U; ++u)
+                        load16<how.value>(logits + s0 + (long)(v + u * 4) * g.B, f[u]);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+                    for (int u = 0; u < U; ++u) {
 #pragma unroll
-                for (int k = 0; k < VEC; ++k)
-                    f[u][k] = grad_of(f[u][k], c[k]);
-                if constexpr (VEC > 1)
-                    store16(dlogits + s0 + (long)(v + u * 4) * g.B, f[u], g.past);
-                else
-                    vec<TS, VEC>::store(dlogits + s0 + (long)(v + u * 4) * g.B, f[u]);
-            }
-        }
+                        for (int k = 0; k < VEC; ++k)
+                            f[u][k] = grad_of(f[u][k], c[k]);
+                        store16<PAST>(dlogits + s0 + (long)(v + u * 4) * g.B, f[u]);
+                    }
+                }
+            });
         for (; v < p.v1; v += 4) {
-            vec<TS, VEC>::load(logits + s0 + (long)v * g.B, f[0]);
+            const long at = s0 + (long)v * g.B;
+            if (nb == VEC)
+                load16(logits + at, f[0]);
+            else
+                load_part(logits + at, 0, nb, f[0], 0.f);
 #pragma unroll
             for (int k = 0; k < VEC; ++k)
                 f[0][k] = grad_of(f[0][k], c[k]);
-            vec<TS, VEC>::store(dlogits + s0 + (long)v * g.B, f[0]);
+            if (nb == VEC)
+                store16(dlogits + at, f[0]);
+            else
+                store_part(dlogits + at, 0, nb, f[0]);
         }
     }
     __syncthreads();
@@ -516,9 +526,10 @@ long stat_groups(int T, int B, int V, int es) {
 // all of it through the cache 233, all past it 238.
 constexpr long KEEP_BYTES = 224L << 20;
 
-// The cut for vectors of VEC elements.
-Cut cut_of(int T, int B, int V, int es, int VEC, int mis, long groups) {
-    Cut g = {T, V, B, V, 1, 0, 1, (long)T * V * B * es >= STREAM_BYTES, 0, mis};
+// The cut of logits whose elements have es bytes.
+Cut cut_of(int T, int B, int V, int es, int mis, long groups) {
+    const int VEC = 16 / es;
+    Cut g = {T, V, B, V, 1, 0, 1, 0, mis};
     const int repeat = B / std::gcd(B, VEC);
     if (repeat <= NT)
         g.lanes = NT / repeat * repeat;
@@ -564,17 +575,21 @@ LossWs layout(void *ws, int T, int B, size_t chunks) {
     return w;
 }
 
-template <typename TS, int VEC>
-hipError_t run(const LossArgs &a, Cut g, const LossWs &w, hipStream_t s) {
+template <typename TS>
+hipError_t run(const LossArgs &a, hipStream_t s) {
+    constexpr int ES = st<TS>::bytes;
+    const int mis = (int)((uintptr_t)a.logits / ES % vec_of<TS>());
+    Cut g = cut_of(a.T, a.B, a.V, ES, mis, stat_groups(a.T, a.B, a.V, ES));
+    const LossWs w = layout(a.ws, a.T, a.B, g.chunks);
     const TS *x = (const TS *)a.logits;
     TS *y = (TS *)a.dlogits;
     hipError_t e;
     const unsigned grid = (unsigned)((long)g.T * g.chunks * g.windows);
     const unsigned flat = (unsigned)(ceil_div(std::max(g.lanes, 1), 64) * 64);
     if (g.lanes)
-        hipLaunchKernelGGL((stat_flat_kernel<TS, VEC>), dim3(grid), dim3(flat), 0, s, g, x, w.stat);
+        hipLaunchKernelGGL((stat_flat_kernel<TS>), dim3(grid), dim3(flat), 0, s, g, x, w.stat);
     else
-        hipLaunchKernelGGL((stat_wide_kernel<TS, VEC>), dim3(grid), dim3(NT), 0, s, g, x, w.stat);
+        hipLaunchKernelGGL((stat_wide_kernel<TS>), dim3(grid), dim3(NT), 0, s, g, x, w.stat);
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
     hipLaunchKernelGGL(token_kernel, dim3((unsigned)w.parts), dim3(NT), 0, s, a, g.chunks, w.stat, w.coef, w.dtarget,
@@ -587,44 +602,24 @@ hipError_t run(const LossArgs &a, Cut g, const LossWs &w, hipStream_t s) {
             hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(NT), 0, s, o);
         return hipGetLastError();
     }
-    g = cut_of(g.T, g.B, g.V, st<TS>::bytes, VEC, g.mis, GRAD_GROUPS);
+    g = cut_of(g.T, g.B, g.V, ES, mis, GRAD_GROUPS);
     const unsigned pieces = (unsigned)((long)g.T * g.chunks * g.windows);
-    if (g.lanes)
-        hipLaunchKernelGGL((grad_flat_kernel<TS, VEC>), dim3(pieces), dim3(flat), 0, s, g, x, y, a.targets, w.coef,
-                           w.dtarget, o);
-    else
-        hipLaunchKernelGGL((grad_wide_kernel<TS, VEC>), dim3(pieces), dim3(NT), 0, s, g, x, y, a.targets, w.coef,
-                           w.dtarget, o);
+    const bool past = (long)g.T * g.V * g.B * ES >= STREAM_BYTES;
+    const auto kernel = g.lanes ? (past ? grad_flat_kernel<TS, true> : grad_flat_kernel<TS, false>)
+                                : (past ? grad_wide_kernel<TS, true> : grad_wide_kernel<TS, false>);
+    hipLaunchKernelGGL(kernel, dim3(pieces), dim3(g.lanes ? flat : NT), 0, s, g, x, y, a.targets, w.coef, w.dtarget, o);
     return hipGetLastError();
-}
-
-// Vectors where the logits and their gradient lie alike to the 16 bytes and,
-// for rows wider than a work-group, every row does; else single elements.
-template <typename TS>
-hipError_t dispatch(const LossArgs &a, hipStream_t s) {
-    constexpr int VEC = vec_of<TS>(), ES = st<TS>::bytes;
-    const int mis = (int)((uintptr_t)a.logits / ES % VEC);
-    const long groups = stat_groups(a.T, a.B, a.V, ES);
-    const bool alike = !a.dlogits || (int)((uintptr_t)a.dlogits / ES % VEC) == mis;
-    Cut g = cut_of(a.T, a.B, a.V, ES, VEC, mis, groups);
-    if (alike && (g.lanes || (mis == 0 && a.B % VEC == 0)))
-        return run<TS, VEC>(a, g, layout(a.ws, a.T, a.B, g.chunks), s);
-    g = cut_of(a.T, a.B, a.V, ES, 1, 0, groups);
-    return run<TS, 1>(a, g, layout(a.ws, a.T, a.B, g.chunks), s);
 }
 
 } // namespace
 
-// For either cut: where the tensors start is not known here.
 size_t loss_ws(int T, int B, int V, bool bf16) {
     const int es = bf16 ? 2 : 4;
-    const long groups = stat_groups(T, B, V, es);
-    const int a = cut_of(T, B, V, es, 16 / es, 0, groups).chunks, b = cut_of(T, B, V, es, 1, 0, groups).chunks;
-    return layout(nullptr, T, B, (size_t)std::max(a, b)).bytes;
+    return layout(nullptr, T, B, (size_t)cut_of(T, B, V, es, 0, stat_groups(T, B, V, es)).chunks).bytes;
 }
 
 hipError_t launch_loss(const LossArgs &a, hipStream_t s) {
-    return a.bf16 ? dispatch<bf16_t>(a, s) : dispatch<float>(a, s);
+    return a.bf16 ? run<bf16_t>(a, s) : run<float>(a, s);
 }
 
 } // namespace lstmss
