@@ -190,19 +190,24 @@ __global__ __launch_bounds__(NT) void stat_flat_kernel(Cut g, const TS *logits, 
             part[j * VEC + k] = {m[k], s[k]};
     }
     __syncthreads();
-    // entry q is of column (c0 + q) mod B; `reps` entries of each, joined by `helpers` threads
-    const int c0 = column_of(g, p, first), reps = g.lanes * VEC / g.B;
-    const int helpers = max(1, min(reps, (int)blockDim.x / g.B));
-    for (int b = j; b < g.B * helpers; b += blockDim.x) {
-        const int h = b / g.B, q0 = (b - h * g.B + g.B - c0) % g.B;
-        Stat a = part[q0 + h * g.B];
-        for (int i = h + helpers; i < reps; i += helpers)
-            a = stat_join(a, part[q0 + i * g.B]);
-        part[q0 + h * g.B] = a;
+    // entry q is of column (c0 + q) mod B: `n` entries of each, B apart, which
+    // rounds of joins of four or more bring down to one
+    const int c0 = column_of(g, p, first);
+    for (int n = g.lanes * VEC / g.B; n > 1;) {
+        const int left = max(1, min((int)blockDim.x / g.B, (n + 3) / 4));
+        for (int b = j; b < g.B * left; b += blockDim.x) { // entries 0 .. left - 1 of every column
+            Stat a = part[b];
+            for (int i = b + left * g.B; i < n * g.B; i += left * g.B)
+                a = stat_join(a, part[i]);
+            part[b] = a;
+        }
+        n = left;
+        __syncthreads();
     }
-    __syncthreads();
-    for (int b = j; b < g.B; b += blockDim.x)
-        stat[((long)p.t * g.chunks + p.c) * g.B + b] = stat_join(part + (b + g.B - c0) % g.B, helpers, g.B);
+    for (int b = j; b < g.B; b += blockDim.x) {
+        const int c = c0 + b; // the column of entry b
+        stat[((long)p.t * g.chunks + p.c) * g.B + (c >= g.B ? c - g.B : c)] = part[b];
+    }
 }
 
 template <typename TS>
