@@ -10,8 +10,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "liblstmss.so")
-SOURCES = ["lstmss_api.cpp", "cell.hip", "gemm1.hip", "gemm1_big.hip", "gemm1_f32.hip", "wgrad_f32.hip", "wgrad_bf16.hip", "gemm.hip",
-           "train.hip", "bidir.hip", "noalloc.hip", "language_api.cpp", "embed.hip", "dropout.hip", "vocab_loss.hip"]
+SOURCES = ["language_api.cpp",  # (takes in lstmss_api.cpp)
+           "cell.hip", "gemm1.hip", "gemm1_big.hip", "gemm1_f32.hip", "wgrad_f32.hip", "wgrad_bf16.hip", "gemm.hip",
+           "train.hip", "bidir.hip", "noalloc.hip", "embed.hip", "dropout.hip", "vocab_loss.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 

@@ -1,33 +1,17 @@
 // Host side of the language-model operators: argument checks and launches.
-#include <hip/hip_runtime.h>
+//
+// One translation unit with the layers' entry points: the calling thread's
+// error message and the timing records are theirs, and these calls set them too.
+#include "lstmss_api.cpp"
 
-#include <cmath>
-#include <cstdarg>
-#include <cstdio>
-
-#include "../../include/lstmss.h"
-#include "host.h"
 #include "language.h"
 
-using namespace lstmss;
-
 namespace {
-
-int32_t fail(int32_t code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
-int32_t fail(int32_t code, const char *fmt, ...) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof(buf), fmt, ap);
-    va_end(ap);
-    return api_fail(code, buf);
-}
 
 // Runs f(), which enqueues a call's kernels, under the timing hooks.
 template <class F>
 int32_t enqueue(const char *what, void *stream, F &&f) {
-    const hipError_t e = api_timed(
-        LSTMSS_KERNEL_AUX, (hipStream_t)stream, [](const void *p) { return (*(const F *)p)(); }, &f);
+    const hipError_t e = timed(LSTMSS_KERNEL_AUX, (hipStream_t)stream, f);
     if (e != hipSuccess)
         return fail(LSTMSS_ERR_HIP, "%s failed: %s", what, hipGetErrorString(e));
     return LSTMSS_OK;

@@ -14,7 +14,6 @@
 #include <vector>
 
 #include "../../include/lstmss.h"
-#include "host.h"
 #include "kernels.h"
 
 using namespace lstmss;
@@ -221,20 +220,6 @@ hipError_t stack_res(StackRes **out) {
     *out = &r;
     return hipSuccess;
 }
-
-} // namespace
-
-namespace lstmss {
-
-int32_t api_fail(int32_t code, const char *text) { return fail(code, "%s", text); }
-
-hipError_t api_timed(int kind, hipStream_t s, hipError_t (*launch)(const void *), const void *arg) {
-    return timed(kind, s, [&] { return launch(arg); });
-}
-
-} // namespace lstmss
-
-namespace {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 long ceil_div(long a, long b) { return (a + b - 1) / b; }
