@@ -451,7 +451,9 @@ def test_embed_of_large_tensors(L, dtype, T, B, I, p):
 
 
 @pytest.mark.parametrize("T,B,I,V,p", [(50, 128, 2048, 4000, 0.0), (50, 128, 2048, 4000, 0.3), (60, 64, 1500, 900, 0.0),
-                                       (16, 96, 1100, 500, 0.2), (1, 1900, 2100, 300, 0.0), (70, 30, 1020, 40, 0.0)])
+                                       (16, 96, 1100, 500, 0.2), (1, 1900, 2100, 300, 0.0), (70, 30, 1020, 40, 0.0),
+                                       (100, 2048, 8, 1000000, 0.0), (2, 40000, 16, 5, 0.3), (40000, 1, 33, 70, 0.0),
+                                       (1, 1, 30000, 1000, 0.5)])
 def test_embed_grad_of_large_tensors(L, T, B, I, V, p):
     rng = np.random.default_rng(I)
     tok = up(tokens_of(rng, T, B, V, "zipf"), torch.int32)
