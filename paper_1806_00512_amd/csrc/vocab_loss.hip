@@ -5,8 +5,9 @@
 //   dL/dx_v = dlogp * ([v = y] - exp(x_v - lse)),  lse = m + log s
 //
 // Three kernels: partial (m, s) of every column over a chunk of rows; the
-// per-token terms (the chunks' joined (m, s), logp, loss term, dlogp); the
-// gradient, one of whose work-groups also sums the loss.  The gradient's
+// per-token terms (the chunks' joined (m, s), logp, loss term, dlogp), which for
+// small logits are one; the gradient, one of whose work-groups also sums the
+// loss.  The gradient's
 // work-groups go through the logits from the end, where the first kernel left
 // off: what of them is still in the last-level cache need not come from memory
 // again.  A step's logits are V * B elements in one piece, columns
@@ -275,6 +276,74 @@ struct Coef {
     float lse, p;
 };
 
+// What a token's terms are made of beside its column's (m, s): x is the
+// target's logit.
+struct TokenIn {
+    int y;
+    float x, w, old, ref, adv;
+};
+
+__device__ __forceinline__ TokenIn token_in(const LossArgs &a, int t, int b) {
+    const long n = (long)t * a.B + b;
+    TokenIn i = {a.targets[n], 0.f, 1.f, 0.f, 0.f, 0.f};
+    if (a.weights)
+        i.w = a.weights[n];
+    if (a.old_logp)
+        i.old = a.old_logp[n];
+    if (a.ref_logp)
+        i.ref = a.ref_logp[n];
+    if (a.adv)
+        i.adv = a.adv[n];
+    if ((uint32_t)i.y < (uint32_t)a.V) {
+        const long at = ((long)t * a.V + i.y) * a.B + b;
+        i.x = a.bf16 ? st<bf16_t>::load((const bf16_t *)a.logits, at) : ((const float *)a.logits)[at];
+    }
+    return i;
+}
+
+// A token's logp, and what the gradient kernel needs of it, written; its loss
+// term, in fp64.
+__device__ __forceinline__ double token_terms(const LossArgs &a, Stat q, const TokenIn &i, long n, Coef *coef,
+                                              float *dtarget) {
+    double term = 0.0, lp = 0.0, g = 0.0;
+    Coef c = {0.f, 0.f};
+    float dt = 0.f;
+    if ((uint32_t)i.y < (uint32_t)a.V && i.w != 0.f) {
+        const double ls = log((double)q.s), lse = (double)q.m + ls;
+        lp = ((double)i.x - (double)q.m) - ls;
+        if (a.mode == LOSS_XENT) {
+            term = -lp;
+            g = -1.0;
+        } else if (a.mode == LOSS_POLICY) {
+            const double A = i.adv;
+            const double r = a.old_logp ? exp(lp - (double)i.old) : 1.0;
+            const double cl = fmin(fmax(r, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high);
+            const double gain = r * A, held = cl * A;
+            const bool open = gain <= held || gain != gain;
+            term = -(open ? gain : held);
+            g = open ? -gain : 0.0;
+            if (a.ref_logp) {
+                const double d = (double)i.ref - lp, e = expm1(d);
+                term += (double)a.kl * (e - d);
+                g -= (double)a.kl * e;
+            }
+        }
+        term *= (double)i.w * (double)a.scale;
+        g *= (double)i.w * (double)a.scale;
+        if (g != 0.0) {
+            // lse's rounding is made good in p, to first order (its square is below 2^-48)
+            c.lse = (float)lse;
+            c.p = (float)(-g * (1.0 + ((double)c.lse - lse)));
+            dt = (float)(-g * expm1(lp));
+        }
+    }
+    if (a.logp)
+        a.logp[n] = (float)lp;
+    coef[n] = c;
+    dtarget[n] = dt;
+    return term;
+}
+
 // 16 tokens to a work-group, 16 threads to a token: they join its chunks, and
 // one of them does its terms in fp64, on operands read while the chunks were.
 // Bound by latency: 3 us for 700 tokens, 5 for 6400.
@@ -287,23 +356,9 @@ __global__ __launch_bounds__(NT) void token_kernel(LossArgs a, int chunks, const
     const int j = threadIdx.x % TOKENS, sub = threadIdx.x / TOKENS;
     const long N = (long)a.T * a.B, n = (long)blockIdx.x * TOKENS + j;
     const int t = (int)(n / a.B), b = (int)(n - (long)t * a.B);
-    int y = -1;
-    float x = 0.f, w = 1.f, old = 0.f, ref = 0.f, adv = 0.f;
-    if (sub == 0 && n < N) {
-        y = a.targets[n];
-        if (a.weights)
-            w = a.weights[n];
-        if (a.old_logp)
-            old = a.old_logp[n];
-        if (a.ref_logp)
-            ref = a.ref_logp[n];
-        if (a.adv)
-            adv = a.adv[n];
-        if ((uint32_t)y < (uint32_t)a.V) {
-            const long at = ((long)t * a.V + y) * a.B + b;
-            x = a.bf16 ? st<bf16_t>::load((const bf16_t *)a.logits, at) : ((const float *)a.logits)[at];
-        }
-    }
+    TokenIn i = {-1};
+    if (sub == 0 && n < N)
+        i = token_in(a, t, b);
     Stat q = {-FLT_MAX, 0.f};
     if (n < N)
         for (int c = sub; c < chunks; c += SUBS * U) {
@@ -321,51 +376,91 @@ __global__ __launch_bounds__(NT) void token_kernel(LossArgs a, int chunks, const
     __syncthreads();
     if (threadIdx.x >= TOKENS)
         return;
-    q = stat_join(&join[0][j], NT / 64, TOKENS);
     double term = 0.0;
-    if (n < N) {
-        double lp = 0.0, g = 0.0;
-        Coef c = {0.f, 0.f};
-        float dt = 0.f;
-        if ((uint32_t)y < (uint32_t)a.V && w != 0.f) {
-            const double ls = log((double)q.s), lse = (double)q.m + ls;
-            lp = ((double)x - (double)q.m) - ls;
-            if (a.mode == LOSS_XENT) {
-                term = -lp;
-                g = -1.0;
-            } else if (a.mode == LOSS_POLICY) {
-                const double A = adv;
-                const double r = a.old_logp ? exp(lp - (double)old) : 1.0;
-                const double cl = fmin(fmax(r, 1.0 - (double)a.clip_low), 1.0 + (double)a.clip_high);
-                const double gain = r * A, held = cl * A;
-                const bool open = gain <= held || gain != gain;
-                term = -(open ? gain : held);
-                g = open ? -gain : 0.0;
-                if (a.ref_logp) {
-                    const double d = (double)ref - lp, e = expm1(d);
-                    term += (double)a.kl * (e - d);
-                    g -= (double)a.kl * e;
-                }
-            }
-            term *= (double)w * (double)a.scale;
-            g *= (double)w * (double)a.scale;
-            if (g != 0.0) {
-                // lse's rounding is made good in p, to first order (its square is below 2^-48)
-                c.lse = (float)lse;
-                c.p = (float)(-g * (1.0 + ((double)c.lse - lse)));
-                dt = (float)(-g * expm1(lp));
-            }
-        }
-        if (a.logp)
-            a.logp[n] = (float)lp;
-        coef[n] = c;
-        dtarget[n] = dt;
-    }
+    if (n < N)
+        term = token_terms(a, stat_join(&join[0][j], NT / 64, TOKENS), i, n, coef, dtarget);
 #pragma unroll
     for (int m = TOKENS / 2; m >= 1; m >>= 1)
         term += __shfl_xor(term, m, 64);
     if (threadIdx.x == 0)
         part[blockIdx.x] = term;
+}
+
+// Sums and terms in one launch, for small logits: a work-group takes VEC columns
+// of a step through all its rows.  The work-groups of a step read the same
+// lines, so they go to one XCD (every eighth) while there are eight steps.
+// Bound by latency, 5 to 6 us.
+constexpr int NARROW_NT = 1024;
+
+template <typename TS>
+__global__ __launch_bounds__(NARROW_NT) void narrow_kernel(LossArgs a, int groups, Coef *coef, float *dtarget, double *part) {
+    constexpr int VEC = vec_of<TS>(), U = 32 / VEC, WAVES = NARROW_NT / 64, SUBS = WAVES / VEC;
+    __shared__ Stat each[VEC][NARROW_NT];
+    __shared__ Stat join[VEC][SUBS];
+    int t, g;
+    if (a.T >= 8) {
+        const int q = blockIdx.x / 8;
+        t = blockIdx.x % 8 + q / groups * 8;
+        g = q % groups;
+        if (t >= a.T)
+            return;
+    } else {
+        t = blockIdx.x / groups;
+        g = blockIdx.x % groups;
+    }
+    const int b0 = g * VEC, nb = min(VEC, a.B - b0), j = threadIdx.x;
+    TokenIn in = {-1};
+    if (j < nb)
+        in = token_in(a, t, b0 + j);
+    const TS *x = (const TS *)a.logits + (long)t * a.V * a.B + b0;
+    float m[VEC], s[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        m[k] = -FLT_MAX;
+        s[k] = 0.f;
+    }
+    for (int v = j; v < a.V; v += U * NARROW_NT) {
+        float f[U][VEC];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int r = v + u * NARROW_NT;
+            if (r < a.V && nb == VEC)
+                load16(x + (long)r * a.B, f[u]);
+            else
+                load_part(x + (long)r * a.B, 0, r < a.V ? nb : 0, f[u], -INFINITY);
+        }
+        stat_add<U, VEC>(f, m, s);
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+        each[k][j] = {m[k], s[k]};
+    __syncthreads();
+    // SUBS waves to a column
+    {
+        const int k = (j >> 6) % VEC, sub = (j >> 6) / VEC;
+        Stat q = stat_join(&each[k][sub * 64 + (j & 63)], NARROW_NT / (64 * SUBS), 64 * SUBS);
+        float top = q.m;
+#pragma unroll
+        for (int w = 32; w >= 1; w >>= 1)
+            top = fmaxf(top, __shfl_xor(top, w, 64));
+        float sum = q.s * __expf(q.m - top);
+#pragma unroll
+        for (int w = 32; w >= 1; w >>= 1)
+            sum += __shfl_xor(sum, w, 64);
+        if ((j & 63) == 0)
+            join[k][sub] = {top, sum};
+    }
+    __syncthreads();
+    if (j >= VEC)
+        return;
+    double term = 0.0;
+    if (j < nb)
+        term = token_terms(a, stat_join(join[j], SUBS, 1), in, (long)t * a.B + b0 + j, coef, dtarget);
+#pragma unroll
+    for (int w = VEC / 2; w >= 1; w >>= 1)
+        term += __shfl_xor(term, w, 64);
+    if (j == 0)
+        part[t * groups + g] = term;
 }
 
 // The loss: the token kernel's partial sums in a fixed order, by one
@@ -569,6 +664,20 @@ Cut cut_of(int T, int B, int V, int es, int mis, long groups) {
     return g;
 }
 
+// Groups of columns of a step where narrow_kernel takes the logits, else 0.  A
+// work-group needs two rounds of loads in fp32, one in bf16 at most, and what
+// the L2 of an XCD gives its work-groups, whole lines, is limited, more so where
+// a step's work-groups are spread over the XCDs.  us of the targets' logp with
+// and without it: 1 x 10000 x 16 fp32 8.0, 8.8; 16 x 5000 x 16 6.5, 8.9; 100 x 10000 x 4
+// 7.8, 8.8; 1 x 1000 x 256 bf16 6.6, 8.8; but 1 x 10000 x 64 fp32 9.5, 8.8, 1 x 5000 x 256
+// 14.0, 8.8, 1 x 32000 x 16 11.3, 8.6, and 1 x 10000 x 16 bf16 10.1, 8.8.
+int narrow_groups(int T, int B, int V, int es) {
+    const long g = ceil_div(B, 16 / es), line = std::min(128L, (long)B * es);
+    const bool rounds = V <= (es == 4 ? 16384 : 4096);
+    const long most = T >= 8 ? 3L << 20 : 3L << 19;
+    return rounds && T * g <= 1024 && ceil_div(T * g, 8) * V * line <= most ? (int)g : 0;
+}
+
 struct LossWs {
     Stat *stat;
     Coef *coef;
@@ -578,14 +687,14 @@ struct LossWs {
     int parts;
 };
 
-LossWs layout(void *ws, int T, int B, size_t chunks) {
+LossWs layout(void *ws, int T, int B, size_t chunks, int groups) {
     const size_t N = (size_t)T * B;
     char *p = (char *)ws;
     LossWs w;
-    w.parts = (int)((N + TOKENS - 1) / TOKENS);
+    w.parts = groups ? T * groups : (int)((N + TOKENS - 1) / TOKENS);
     size_t at = 0;
     w.stat = (Stat *)(p + at);
-    at += align256(N * chunks * sizeof(Stat));
+    at += groups ? 0 : align256(N * chunks * sizeof(Stat));
     w.coef = (Coef *)(p + at);
     at += align256(N * sizeof(Coef));
     w.dtarget = (float *)(p + at);
@@ -601,20 +710,26 @@ hipError_t run(const LossArgs &a, hipStream_t s) {
     constexpr int ES = st<TS>::bytes;
     const int mis = (int)((uintptr_t)a.logits / ES % vec_of<TS>());
     Cut g = cut_of(a.T, a.B, a.V, ES, mis, stat_groups(a.T, a.B, a.V, ES));
-    const LossWs w = layout(a.ws, a.T, a.B, g.chunks);
+    const int groups = narrow_groups(a.T, a.B, a.V, ES);
+    const LossWs w = layout(a.ws, a.T, a.B, g.chunks, groups);
     const TS *x = (const TS *)a.logits;
     TS *y = (TS *)a.dlogits;
     hipError_t e;
     const unsigned grid = (unsigned)((long)g.T * g.chunks * g.windows);
     const unsigned flat = (unsigned)(ceil_div(std::max(g.lanes, 1), 64) * 64);
-    if (g.lanes)
-        hipLaunchKernelGGL((stat_flat_kernel<TS>), dim3(grid), dim3(flat), 0, s, g, x, w.stat);
-    else
-        hipLaunchKernelGGL((stat_wide_kernel<TS>), dim3(grid), dim3(NT), 0, s, g, x, w.stat);
-    if ((e = hipGetLastError()) != hipSuccess)
-        return e;
-    hipLaunchKernelGGL(token_kernel, dim3((unsigned)w.parts), dim3(NT), 0, s, a, g.chunks, w.stat, w.coef, w.dtarget,
-                       w.part);
+    if (groups) {
+        const unsigned steps = a.T >= 8 ? (unsigned)ceil_div(a.T, 8) * 8 : (unsigned)a.T;
+        hipLaunchKernelGGL(narrow_kernel<TS>, dim3(steps * groups), dim3(NARROW_NT), 0, s, a, groups, w.coef, w.dtarget, w.part);
+    } else {
+        if (g.lanes)
+            hipLaunchKernelGGL((stat_flat_kernel<TS>), dim3(grid), dim3(flat), 0, s, g, x, w.stat);
+        else
+            hipLaunchKernelGGL((stat_wide_kernel<TS>), dim3(grid), dim3(NT), 0, s, g, x, w.stat);
+        if ((e = hipGetLastError()) != hipSuccess)
+            return e;
+        hipLaunchKernelGGL(token_kernel, dim3((unsigned)w.parts), dim3(NT), 0, s, a, g.chunks, w.stat, w.coef, w.dtarget,
+                           w.part);
+    }
     if ((e = hipGetLastError()) != hipSuccess)
         return e;
     const LossOut o = {w.part, w.parts, a.loss};
@@ -636,7 +751,8 @@ hipError_t run(const LossArgs &a, hipStream_t s) {
 
 size_t loss_ws(int T, int B, int V, bool bf16) {
     const int es = bf16 ? 2 : 4;
-    return layout(nullptr, T, B, (size_t)cut_of(T, B, V, es, 0, stat_groups(T, B, V, es)).chunks).bytes;
+    return layout(nullptr, T, B, (size_t)cut_of(T, B, V, es, 0, stat_groups(T, B, V, es)).chunks,
+                  narrow_groups(T, B, V, es)).bytes;
 }
 
 hipError_t launch_loss(const LossArgs &a, hipStream_t s) {

@@ -207,6 +207,25 @@ def test_embed_grad(L, T, B, I, V, kind, p, accumulate, skip):
     assert torch.equal(dE, first)
 
 
+@pytest.mark.parametrize("T,B,I", [(3, 64, 70), (40, 64, 66), (2, 20, 30), (33, 100, 12)])
+@pytest.mark.parametrize("period", [1, 13, 100, 1000003])
+def test_masks_that_repeat_after_any_length(L, T, B, I, period):
+    """Lookup and gradient with masks that repeat after no multiple of eight, few positions and many."""
+    rng = np.random.default_rng(period)
+    V = 40
+    tok = tokens_of(rng, T, B, V, "some")
+    E = rng.standard_normal((V, I)).astype(np.float32)
+    g = rng.standard_normal((T, I, B)).astype(np.float32)
+    drop = L.drop(0.4, 21, 16, period)
+    x = L.embed(up(tok, torch.int32), up(E), drop=drop)
+    k = O.keep(x.numel(), 0.4, 21, 16, period).reshape(T, I, B)
+    ref = np.where(k, O.embed(tok, E).astype(np.float32) * np.float32(O.keep_scale(0.4)), np.float32(0))
+    assert torch.equal(x, up(ref))
+    dE = L.embed_grad(up(tok, torch.int32), up(g), V, drop=drop)
+    want, count, size = O.embed_grad(tok, O.dropout(g, 0.4, 21, 16, period), V)
+    assert (np.abs(np64(dE) - want) <= (count[:, None] + 3) * U * size).all()
+
+
 def test_embed_grad_against_differences(L):
     """<G, embed(E)> differs between E + h and E - h by 2 h <G, embed'>: linear, so any h."""
     rng = np.random.default_rng(3)
@@ -472,15 +491,23 @@ def test_embed_grad_of_large_tensors(L, T, B, I, V, p):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,V,B", [(2, 20000, 250), (3, 9999, 333), (2, 30000, 640), (4, 40000, 500), (1, 30011, 2100),
-                                   (31, 32001, 128)])
-def test_xent_of_large_tensors(L, dtype, T, V, B):
-    """From 32 MB on the gradient is written another way, from 224 MB on part of the logits is
-    read another way: against the same formula in fp64, step by step."""
+                                   (31, 32001, 128), (33, 17001, 3), (5, 16411, 20), (1, 20001, 1), (2, 17003, 130),
+                                   (40, 4999, 33), (100, 2000, 33), (12, 16500, 7), (1, 17000, 2100), (2, 50, 9000),
+                                   (3, 20000, 1031), (300, 1000, 9), (1, 17001, 256), (7, 16400, 255)])
+@pytest.mark.parametrize("skip", [(0, 0), (1, 1), (3, 6)])
+def test_xent_of_large_tensors(L, dtype, T, V, B, skip):
+    """Small logits take one kernel for sums and terms, larger ones two; from 32 MB on the gradient
+    is written another way, from 224 MB on part of the logits is read another way: against the same
+    formula in fp64, step by step, with tensors that start anywhere."""
     g = torch.Generator(device=DEV)
     g.manual_seed(V)
-    x = (torch.randn((T, V, B), generator=g, device=DEV) * 3).to(TYPES[dtype])
+    whole, x = odd_start((T, V, B), TYPES[dtype], skip[0])
+    x.copy_(torch.randn((T, V, B), generator=g, device=DEV) * 3)
     y = torch.randint(-1, V, (T, B), generator=g, device=DEV, dtype=torch.int32)
-    out = L.xent(x, y, scale=0.5)
+    whole, d = odd_start((T, V, B), TYPES[dtype], skip[1])
+    out = L.xent(x, y, scale=0.5, out={"dlogits": d})
+    guards_hold(whole, skip[1], d.numel())
+    assert abs(float(out["loss"]) + 0.5 * float(out["logp"].double().sum())) <= 4 * U * 0.5 * float(out["logp"].double().abs().sum())
     for t in range(T):
         lsm = torch.log_softmax(x[t].double(), 0)
         on = (y[t] >= 0).double()
@@ -489,10 +516,10 @@ def test_xent_of_large_tensors(L, dtype, T, V, B):
         tol = U * (16 * np.sqrt(V) + 16 + 2 * lp.abs())
         assert ((out["logp"][t].double() - lp).abs() <= tol).all()
         p = lsm.exp()
-        d = 0.5 * on * p
-        d[at, torch.arange(B, device=DEV)] -= 0.5 * on
-        lim = 0.5 * on * p * (tol + (3 * lsm.abs() + 16) * U) + 2 * U * 0.5 + d.abs() * (2.0**-8 if dtype == "bf16" else 2 * U) + 2.0**-133
-        assert ((out["dlogits"][t].double() - d).abs() <= lim).all()
+        ref = 0.5 * on * p
+        ref[at, torch.arange(B, device=DEV)] -= 0.5 * on
+        lim = 0.5 * on * p * (tol + (3 * lsm.abs() + 16) * U) + 2 * U * 0.5 + ref.abs() * (2.0**-8 if dtype == "bf16" else 2 * U) + 2.0**-133
+        assert ((d[t].double() - ref).abs() <= lim).all()
 
 
 # ------------------------------------------------------------ calls
