@@ -236,12 +236,21 @@ __global__ __launch_bounds__(SORT_NT) void sort_kernel(const int32_t *tokens, in
     __syncthreads();
     const int share = (int)(ceil_div(N, SORT_NT) * 64);
     const int p0 = (int)min((long)N, (long)w * share), p1 = (int)min((long)N, (long)p0 + share);
+    // loads on their way together: 25600 positions, 8 features, 1000000 rows 66 us
+    // so, 168 one by one, 68 by eights; 700 and 10000 rows alike, but 0.5 slower by eights
+    constexpr int U = 4;
     int before = 0;
-    for (int p = p0 + lane; p < p1; p += 64) {
-        const uint32_t v = (uint32_t)tokens[p];
-        before += v < (uint32_t)lo;
-        if (v - (uint32_t)lo < (uint32_t)n)
-            atomicAdd(&hist[w][v - lo], 1);
+    for (int p = p0 + lane; p < p1; p += 64 * U) {
+        uint32_t v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            v[u] = p + u * 64 < p1 ? (uint32_t)tokens[p + u * 64] : ~0u;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            before += v[u] < (uint32_t)lo;
+            if (v[u] - (uint32_t)lo < (uint32_t)n)
+                atomicAdd(&hist[w][v[u] - lo], 1);
+        }
     }
     for (int m = 32; m >= 1; m >>= 1)
         before += __shfl_xor(before, m, 64);
@@ -283,22 +292,32 @@ __global__ __launch_bounds__(SORT_NT) void sort_kernel(const int32_t *tokens, in
     volatile int *next = hist[w];
     const int bits = 32 - __clz(R - 1);
     const uint64_t below = (1ull << lane) - 1;
-    for (int base = p0; base < p1; base += 64) {
-        const int p = base + lane;
-        const uint32_t k = (uint32_t)(p < p1 ? tokens[p] : -1) - (uint32_t)lo;
-        const bool in = k < (uint32_t)n;
-        uint64_t same = __ballot(in);
-        for (int j = 0; j < bits; ++j) {
-            const uint64_t one = __ballot(k >> j & 1);
-            same &= k >> j & 1 ? one : ~one;
+    for (int base = p0; base < p1; base += 64 * U) {
+        uint32_t v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int p = base + u * 64 + lane;
+            v[u] = p < p1 ? (uint32_t)tokens[p] : ~0u;
         }
-        if (in) {
-            const int first = next[k], r = first + __popcll(same & below);
-            rank[p] = r;
-            order[r] = p;
-            key[r] = lo + (int)k;
-            if ((same & below) == 0)
-                next[k] = first + __popcll(same);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t k = v[u] - (uint32_t)lo;
+            const bool in = k < (uint32_t)n;
+            uint64_t same = __ballot(in);
+            if (same == 0)
+                continue;
+            for (int j = 0; j < bits; ++j) {
+                const uint64_t one = __ballot(k >> j & 1);
+                same &= k >> j & 1 ? one : ~one;
+            }
+            if (in) {
+                const int p = base + u * 64 + lane, first = next[k], r = first + __popcll(same & below);
+                rank[p] = r;
+                order[r] = p;
+                key[r] = lo + (int)k;
+                if ((same & below) == 0)
+                    next[k] = first + __popcll(same);
+            }
         }
     }
 }
