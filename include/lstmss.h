@@ -321,8 +321,8 @@ int32_t lstmss_mse_grad(const lstmss_dims *d, const void *h, const float *y, flo
  * is zero, it adds to no gradient, its logp, loss and dlogits are zero,
  * whatever its logits hold).
  * Sizes: T steps, batch B, I features of the embedding, vocabulary V; dtype is
- * the storage type of the embedding table and x, or of the logits.  T * B below
- * 2^28, V at most 2^26, V * B, V * I and I * B below 2^31, and
+ * the storage type of the embedding table and x, or of the logits.  T * B at most
+ * 2^28 - 16, V at most 2^26, V * B, V * I and I * B below 2^31, and
  * T * (B / 33 + 1) * (I / 64 + 1) (whole quotients) below 2^23.
  * The loss calls do not use I, which must be positive all the same. */
 typedef struct {

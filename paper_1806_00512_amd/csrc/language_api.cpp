@@ -27,10 +27,10 @@ int32_t check_tokens(const lstmss_tokens *d, bool dtype) {
         return fail(LSTMSS_ERR_UNSUPPORTED, "unknown dtype %d", d->dtype);
     // indices within a step and row numbers fit 32 bits; grids (a work-group for
     // each step and 40 or more of its columns, and for 64 features of these, or
-    // for 16 rows of the table) stay below 2^32 threads
+    // for 16 rows of the table; 256 threads for 16 tokens) stay below 2^32 threads
     const int64_t N = (int64_t)d->T * d->B, m31 = (int64_t)1 << 31;
     const int64_t steps = (int64_t)d->T * (d->B / 33 + 1), tiles = steps * (d->I / 64 + 1);
-    if (N >= (int64_t)1 << 28 || d->V > 1 << 26 || (int64_t)d->V * d->B >= m31 || (int64_t)d->V * d->I >= m31 ||
+    if (N > ((int64_t)1 << 28) - 16 || d->V > 1 << 26 || (int64_t)d->V * d->B >= m31 || (int64_t)d->V * d->I >= m31 ||
         (int64_t)d->I * d->B >= m31 || tiles >= (int64_t)1 << 23)
         return fail(LSTMSS_ERR_UNSUPPORTED, "sizes too large");
     return LSTMSS_OK;

@@ -140,6 +140,15 @@ def test_sizes_refused(L, sizes, code):
     assert lib.lstmss_last_error()
 
 
+def test_most_tokens(L):
+    # the token kernel's grid: 256 threads for 16 tokens, below 2^32 of them
+    most = (1 << 28) - 16
+    lib = L.load()
+    assert lib.lstmss_loss_workspace_bytes(tokens(L, T=1, B=most, I=1, V=1)) > 0
+    for B in range(most + 1, most + 16):
+        assert lib.lstmss_loss_workspace_bytes(tokens(L, T=1, B=B, I=1, V=1)) == -2
+
+
 def test_null_pointers_refused(L):
     lib, d = L.load(), tokens(L)
     q = ctypes.byref(L.Policy(0.2, 0.2, 0.0, 1.0))
