@@ -2,7 +2,7 @@
 // the targets, per-token terms, gradient in the logits.
 //
 //   m = max_v x_v,  s = sum_v exp(x_v - m),  logp = x_y - m - log s
-//   dL/dx_v = dlogp * ([v = y] - exp(x_v - lse)),  lse = m + log s
+//   dL/dx_v = dlogp * ([v = y] - exp(x_v - m) / s)
 //
 // Three kernels: partial (m, s) of every column over a chunk of rows; the
 // per-token terms (the chunks' joined (m, s), logp, loss term, dlogp), which for
@@ -12,7 +12,7 @@
 // off: what of them is still in the last-level cache need not come from memory
 // again.  A step's logits are V * B elements in one piece, columns
 // fastest, so a thread that walks a piece in strides of whole rows keeps its
-// columns: their running (m, s), or their (lse, dlogp), stay in registers,
+// columns: their running (m, s), or their (m, -dlogp / s), stay in registers,
 // whatever B is.
 //
 // Bound by the memory, which gives the logits twice and takes the gradient
@@ -268,12 +268,15 @@ __global__ __launch_bounds__(NT) void stat_wide_kernel(Cut g, const TS *logits, 
             stat[((long)p.t * g.chunks + p.c) * g.B + b + k] = stat_join(part + k * 64 + lane, 4, VEC * 64);
 }
 
-// What the gradient kernel needs of a token: dL/dx_v = p * exp(min(x_v - lse, 1)),
-// p = -dlogp (with what rounding lse to fp32 left out), and the gradient at
-// the target itself.  A token that takes no part has p = 0: the minimum makes
+// What the gradient kernel needs of a token: dL/dx_v = p * exp(min(x_v - m, GROW
+// + 1)), m the reference that its sum s is of and p = -dlogp / s, and the
+// gradient at the target itself.  m is a logit of the column, not m + log s: the
+// difference is exact where the exponential counts, whatever the logits' size,
+// where log s would be lost beside a large m.  A token that takes no part has p =
+// 0: the minimum, which no other token meets (x_v is at most GROW above m), makes
 // its exponentials finite whatever its logits are, so it gets zeros.
 struct Coef {
-    float lse, p;
+    float m, p;
 };
 
 // What a token's terms are made of beside its column's (m, s): x is the
@@ -309,7 +312,7 @@ __device__ __forceinline__ double token_terms(const LossArgs &a, Stat q, const T
     Coef c = {0.f, 0.f};
     float dt = 0.f;
     if ((uint32_t)i.y < (uint32_t)a.V && i.w != 0.f) {
-        const double ls = log((double)q.s), lse = (double)q.m + ls;
+        const double ls = log((double)q.s);
         lp = ((double)i.x - (double)q.m) - ls;
         if (a.mode == LOSS_XENT) {
             term = -lp;
@@ -331,9 +334,8 @@ __device__ __forceinline__ double token_terms(const LossArgs &a, Stat q, const T
         term *= (double)i.w * (double)a.scale;
         g *= (double)i.w * (double)a.scale;
         if (g != 0.0) {
-            // lse's rounding is made good in p, to first order (its square is below 2^-48)
-            c.lse = (float)lse;
-            c.p = (float)(-g * (1.0 + ((double)c.lse - lse)));
+            c.m = q.m;
+            c.p = (float)(-g / (double)q.s);
             dt = (float)(-g * expm1(lp));
         }
     }
@@ -491,7 +493,7 @@ __device__ __forceinline__ void loss_sum(const LossOut &o) {
 
 __global__ __launch_bounds__(NT) void loss_sum_kernel(LossOut o) { loss_sum(o); }
 
-__device__ __forceinline__ float grad_of(float x, Coef c) { return c.p * __expf(fminf(x - c.lse, 1.f)); }
+__device__ __forceinline__ float grad_of(float x, Coef c) { return c.p * __expf(fminf(x - c.m, GROW + 1.f)); }
 
 // The targets' own elements of a piece, written over what the softmax's term
 // alone gave them (same work-group, after a barrier).

@@ -405,6 +405,52 @@ def test_loss_alignment(L, dtype, T, V, B, skip):
     guards_hold(lw, skip, T * B)
 
 
+# T, V, B whose sums are taken by each of the kernels in both types: one launch for sums and
+# terms; whole rows to a work-group; windows of long rows
+OFFSET_SHAPES = [(3, 97, 20), (2, 5003, 33), (1, 20000, 8), (1, 700, 2056), (1, 1300, 1031)]
+
+
+def offset_logits(rng, T, V, B, dtype):
+    """Columns around offsets of every size, and columns that hold one finite value alone (a
+    vocabulary masked out as a whole), as they are stored."""
+    most = torch.finfo(TYPES[dtype]).max
+    spread = [0.0, 1e5, -1e6, 4e6, -1e7, 1e9, -1e9, 1e20]
+    alone = [-1e9, -most, most, 1e9, -1e4, 0.0]
+    x = up(rng.standard_normal((T, V, B)).astype(np.float32) * 3).double()
+    for b in range(B):
+        k = b % (len(spread) + len(alone))
+        if k < len(spread):
+            x[:, :, b] += spread[k]
+        else:
+            x[:, :, b] = alone[k - len(spread)]
+    return x.to(TYPES[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,B", OFFSET_SHAPES)
+def test_gradients_at_any_offset(L, dtype, T, V, B):
+    """What is common to a column takes no part, however large: the bounds are those of logits
+    around zero.  A column of one value alone has the uniform distribution's gradient."""
+    rng = np.random.default_rng(V)
+    x = offset_logits(rng, T, V, B, dtype)
+    y = rng.integers(0, V, (T, B)).astype(np.int32)
+    w = rng.uniform(0.2, 2, (T, B)).astype(np.float32)
+    yt = up(y, torch.int32)
+    loss, logp, g, d = O.xent(np64(x), y, w, 0.25)
+    out = L.xent(x, yt, weights=up(w), scale=0.25)
+    tol = logp_tol(V, logp)
+    assert (np.abs(np64(out["logp"]) - logp) <= tol).all()
+    assert abs(float(out["loss"]) - loss) <= (np.abs(g) * tol).sum() + 2 * U * (abs(loss) + np.abs(g * logp).sum())
+    check_grad(L, out["dlogits"], x, d, g, V, dtype, tol, 2 * U * np.abs(g))
+    # the policy loss, unclipped: r is within [1 - 2^-4, 1 + 2^-4]
+    old = (logp + rng.uniform(-0.06, 0.06, (T, B))).astype(np.float32)
+    ref = (logp + rng.uniform(-0.3, 0.3, (T, B))).astype(np.float32)
+    adv = rng.standard_normal((T, B)).astype(np.float32)
+    out = L.policy_loss(x, yt, up(old), up(ref), up(adv), weights=up(w), kl=0.125, scale=0.25)
+    _, _, g, d = O.policy_loss(np64(x), y, old, ref, adv, w, 0.2, 0.2, 0.125, 0.25)
+    slope = 0.25 * w * (np.abs(adv) * np.exp(0.07) + 0.125 * np.exp(0.31))
+    check_grad(L, out["dlogits"], x, d, g, V, dtype, tol, slope * tol + 4 * U * np.abs(g))
+
 def test_xent_against_differences(L):
     """Central differences of the loss along one direction: h^2 / 6 of its third derivative and
     the loss's rounding over h."""
