@@ -635,10 +635,15 @@ def _sizes(T, B, I, V, dtype) -> Tokens:
 
 
 def _new(shape, dtype, dev, stream):
-    """A tensor that work on `stream` (None: the current one, for which it is allocated) will use."""
-    t = torch.empty(shape, dtype=dtype, device=dev)
-    if stream is not None:
-        t.record_stream(stream)
+    """A tensor that work on `stream` (None: the current one) will use.  It is of that stream's
+    own blocks: one freed on the current stream may still be at work there.  The caller may
+    go on with it on the current stream, and free it, once that waits for `stream`."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    caller = torch.cuda.current_stream(dev)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=dev)
+    t.record_stream(caller)
     return t
 
 

@@ -632,6 +632,22 @@ def test_calls_on_another_stream(L):
     assert torch.equal(own["dlogits"], s["o1"]["dlogits"])
 
 
+def test_new_tensors_of_a_call_on_another_stream(L):
+    """They are not made of blocks that the current stream's work may still use."""
+    d = L.drop(0.5, 7)
+    x = torch.randn(3, 1000, 777, device=DEV)
+    ref = L.dropout(x, d)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    freed = torch.empty_like(x)
+    at = freed.data_ptr()
+    del freed
+    y = L.dropout(x, d, stream=side)
+    side.synchronize()
+    assert y.data_ptr() != at and torch.equal(y, ref)
+    again = torch.empty_like(x)
+    assert again.data_ptr() == at          # it is still the current stream's
+
 def test_calls_in_a_captured_graph(L):
     """Recorded by the caller and replayed, with eager work between: every replay gives the
     eager call's bits."""
