@@ -215,6 +215,19 @@ def _stream(stream):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _new(shape, dtype, dev, stream):
+    """A tensor that work on `stream` (None: the current one) will use.  It is of that stream's
+    own blocks: one freed on the current stream may still be at work there.  The caller may
+    go on with it on the current stream, and free it, once that waits for `stream`."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    caller = torch.cuda.current_stream(dev)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=dev)
+    t.record_stream(caller)
+    return t
+
+
 def cache_bytes(d: Dims) -> int:
     n = load().lstmss_cache_bytes(ctypes.byref(d))
     _check(0 if n >= 0 else int(n), "lstmss_cache_bytes")
@@ -280,11 +293,11 @@ def fwd_cache(x, W, b=None, h0=None, c0=None, h_out=None, cache=None, stream=Non
     st = x.dtype
     d = dims(T, B, I, H, st)
     if cache is None:
-        cache = torch.empty(cache_bytes(d), dtype=torch.uint8, device=x.device)
+        cache = _new(cache_bytes(d), torch.uint8, x.device, stream)
     if h_out is None:
-        h_out = torch.empty((T, H, B), dtype=st, device=x.device)
+        h_out = _new((T, H, B), st, x.device, stream)
     if batched and ws is None:
-        ws = torch.empty(fwd_workspace_bytes(d), dtype=torch.uint8, device=x.device)
+        ws = _new(fwd_workspace_bytes(d), torch.uint8, x.device, stream)
     if not batched:
         ws = None
     rc = load().lstm_fwd_cache(ctypes.byref(d), _ptr(x, st, name="x"),
@@ -321,9 +334,9 @@ def mse_grad(h, y, dH=None, loss=None, stream=None):
     T, H, B = h.shape
     d = dims(T, B, 1, H, h.dtype)
     if dH is None:
-        dH = torch.empty((T, H, B), dtype=torch.float32, device=h.device)
+        dH = _new((T, H, B), torch.float32, h.device, stream)
     if loss is None:
-        loss = torch.empty(LOSS_SLOTS, dtype=torch.float64, device=h.device)
+        loss = _new(LOSS_SLOTS, torch.float64, h.device, stream)
     rc = load().lstmss_mse_grad(ctypes.byref(d), _ptr(h, h.dtype, name="h"),
                                 _ptr(y, torch.float32, (T, H, B), "y"),
                                 _ptr(dH, torch.float32, (T, H, B), "dH"),
@@ -366,17 +379,17 @@ def bwd_stack(xs, Ws, caches, dH_top, sparsity=0.5, P=4, R=8, kind=COARSE, My=0,
     s = structure(P, R, kind, My, Mx) if sparsity > 0 else None
     sp = float(sparsity)
     if dWs is None:
-        dWs = [torch.empty(tuple(W.shape), dtype=f32, device=dev) for W in Ws]
+        dWs = [_new(tuple(W.shape), f32, dev, stream) for W in Ws]
     if dbs is None:
-        dbs = [torch.empty(W.shape[0], dtype=f32, device=dev) for W in Ws]
+        dbs = [_new(W.shape[0], f32, dev, stream) for W in Ws]
     if dXs is None:
-        dXs = [torch.empty(tuple(x.shape), dtype=f32, device=dev) if (l > 0 or want_dX0) else None
+        dXs = [_new(tuple(x.shape), f32, dev, stream) if (l > 0 or want_dX0) else None
                for l, x in enumerate(xs)]
     if idxs is None and s is not None:
-        idxs = [torch.empty((T, index_entries(ds[l], sp, s)), dtype=torch.int32, device=dev)
+        idxs = [_new((T, index_entries(ds[l], sp, s)), torch.int32, dev, stream)
                 for l in range(n)]
     if ws is None:
-        ws = torch.empty(stack_workspace_bytes(list(ds), sp, s), dtype=torch.uint8, device=dev)
+        ws = _new(stack_workspace_bytes(list(ds), sp, s), torch.uint8, dev, stream)
     rc = load().lstm_bwd_stack(
         n, ds, sp, ctypes.byref(s) if s else None, _ptr_array(xs, "x", st),
         _ptr_array(Ws, "W", st), _ptr_array(caches, "cache", torch.uint8),
@@ -390,7 +403,7 @@ def bwd_stack(xs, Ws, caches, dH_top, sparsity=0.5, P=4, R=8, kind=COARSE, My=0,
 def time_reverse(src, dst=None, stream=None):
     """dst[s] = src[T-1-s] along the first dimension (a new tensor unless given)."""
     if dst is None:
-        dst = torch.empty_like(src)
+        dst = _new(src.shape, src.dtype, src.device, stream)
     T = src.shape[0]
     step = src[0].numel() * src.element_size()
     rc = load().lstmss_time_reverse(int(T), int(step), _ptr(src, name="src"),
@@ -404,7 +417,7 @@ def bidir_join(h_fwd, h_rev, out=None, stream=None):
     T, H, B = h_fwd.shape
     d = dims(T, B, 1, H, h_fwd.dtype)
     if out is None:
-        out = torch.empty((T, 2 * H, B), dtype=h_fwd.dtype, device=h_fwd.device)
+        out = _new((T, 2 * H, B), h_fwd.dtype, h_fwd.device, stream)
     rc = load().lstmss_bidir_join(ctypes.byref(d), _ptr(h_fwd, name="h_fwd"),
                                   _ptr(h_rev, h_fwd.dtype, (T, H, B), "h_rev"),
                                   _ptr(out, h_fwd.dtype, (T, 2 * H, B), "out"), _stream(stream))
@@ -427,19 +440,19 @@ def bwd_bidir(x, x_rev, W_fwd, W_rev, cache_fwd, cache_rev, dH_up, sparsity=0.5,
     for k, shape, dt in (("dW_fwd", (4 * H, I + H), f32), ("dW_rev", (4 * H, I + H), f32),
                          ("db_fwd", (4 * H,), f32), ("db_rev", (4 * H,), f32)):
         if o.get(k) is None:
-            o[k] = torch.empty(shape, dtype=dt, device=dev)
+            o[k] = _new(shape, dt, dev, stream)
     if want_dX and o.get("dX") is None:
-        o["dX"] = torch.empty((T, I, B), dtype=f32, device=dev)
+        o["dX"] = _new((T, I, B), f32, dev, stream)
     if s is not None:
         ne = index_entries(d, sparsity, s)
         for k in ("idx_fwd", "idx_rev"):
             if o.get(k) is None:
-                o[k] = torch.empty((T, ne), dtype=torch.int32, device=dev)
+                o[k] = _new((T, ne), torch.int32, dev, stream)
     if ws is None:
         n = load().lstmss_bidir_workspace_bytes(ctypes.byref(d), float(sparsity),
                                                 ctypes.byref(s) if s is not None else None)
         _check(0 if n >= 0 else int(n), "lstmss_bidir_workspace_bytes")
-        ws = torch.empty(int(n), dtype=torch.uint8, device=dev)
+        ws = _new(int(n), torch.uint8, dev, stream)
     rc = load().lstm_bwd_bidir(
         ctypes.byref(d), float(sparsity), ctypes.byref(s) if s is not None else None,
         _ptr(x, st, name="x"), _ptr(x_rev, st, (T, I, B), "x_rev"),
@@ -455,14 +468,14 @@ def bwd_bidir(x, x_rev, W_fwd, W_rev, cache_fwd, cache_rev, dH_up, sparsity=0.5,
     return o
 
 
-def _bwd_outputs(T, B, I, H, dev, want_dX, out):
+def _bwd_outputs(T, B, I, H, dev, want_dX, out, stream):
     out = dict(out or {})
     f32 = torch.float32
     if want_dX and out.get("dX") is None:
-        out["dX"] = torch.empty((T, I, B), dtype=f32, device=dev)
+        out["dX"] = _new((T, I, B), f32, dev, stream)
     for k, shape in (("dW", (4 * H, I + H)), ("db", (4 * H,)), ("dh0", (H, B)), ("dc0", (H, B))):
         if out.get(k) is None:
-            out[k] = torch.empty(shape, dtype=f32, device=dev)
+            out[k] = _new(shape, f32, dev, stream)
     return out
 
 
@@ -473,9 +486,9 @@ def bwd_dense(x, W, cache, dH_up, dhT=None, dcT=None, want_dX=True, out=None, ws
     H = W.shape[0] // 4
     st = x.dtype
     d = dims(T, B, I, H, st)
-    o = _bwd_outputs(T, B, I, H, x.device, want_dX, out)
+    o = _bwd_outputs(T, B, I, H, x.device, want_dX, out, stream)
     if ws is None:
-        ws = torch.empty(workspace_bytes(d, 0.0, None), dtype=torch.uint8, device=x.device)
+        ws = _new(workspace_bytes(d, 0.0, None), torch.uint8, x.device, stream)
     f32 = torch.float32
     rc = load().lstm_bwd_dense(
         ctypes.byref(d), _ptr(x, st, name="x"), _ptr(W, st, (4 * H, I + H), "W"),
@@ -501,14 +514,14 @@ def bwd_structsparse(x, W, cache, dH_up, sparsity=0.5, P=4, R=8, dhT=None, dcT=N
     st = x.dtype
     d = dims(T, B, I, H, st)
     s = structure(P, R, kind, My, Mx)
-    o = _bwd_outputs(T, B, I, H, x.device, want_dX, out)
+    o = _bwd_outputs(T, B, I, H, x.device, want_dX, out, stream)
     ne = index_entries(d, sparsity, s)
     if want_idx and o.get("idx") is None:
-        o["idx"] = torch.empty((T, ne), dtype=torch.int32, device=x.device)
+        o["idx"] = _new((T, ne), torch.int32, x.device, stream)
     if want_dbg and o.get("dbg") is None:
-        o["dbg"] = torch.empty((T, 4 * H, B), dtype=st, device=x.device)
+        o["dbg"] = _new((T, 4 * H, B), st, x.device, stream)
     if ws is None:
-        ws = torch.empty(workspace_bytes(d, sparsity, s), dtype=torch.uint8, device=x.device)
+        ws = _new(workspace_bytes(d, sparsity, s), torch.uint8, x.device, stream)
     f32 = torch.float32
     rc = load().lstm_bwd_structsparse(
         ctypes.byref(d), float(sparsity), ctypes.byref(s), _ptr(x, st, name="x"),
@@ -540,18 +553,18 @@ def select_compact(dG, sparsity=0.5, P=4, R=8, want_scores=True, stream=None, ki
     s = structure(P, R, kind, My, Mx)
     kp = kept_rows(d, sparsity, s)
     ne = index_entries(d, sparsity, s)
-    dGc = torch.empty((kp, B), dtype=st, device=dG.device)
+    dGc = _new((kp, B), st, dG.device, stream)
     if kind == FINE:
         nb = -(-B // My)
-        idx = torch.empty((G // Mx, ne // (G // Mx)), dtype=torch.int32, device=dG.device)
-        sc = (torch.empty((G // Mx, nb), dtype=torch.float64, device=dG.device)
+        idx = _new((G // Mx, ne // (G // Mx)), torch.int32, dG.device, stream)
+        sc = (_new((G // Mx, nb), torch.float64, dG.device, stream)
               if want_scores else None)
     else:
-        idx = torch.empty((ne,), dtype=torch.int32, device=dG.device)
-        sc = (torch.empty((G // P,), dtype=torch.float64, device=dG.device)
+        idx = _new((ne,), torch.int32, dG.device, stream)
+        sc = (_new((G // P,), torch.float64, dG.device, stream)
               if want_scores else None)
     n = select_workspace_bytes(d, sparsity, s)
-    ws = torch.empty(n, dtype=torch.uint8, device=dG.device) if n > 0 else None
+    ws = _new(n, torch.uint8, dG.device, stream) if n > 0 else None
     rc = load().lstmss_select_compact(ctypes.byref(d), float(sparsity), ctypes.byref(s),
                                       _ptr(dG, st, name="dG"), _ptr(dGc), _ptr(idx), _ptr(sc),
                                       _ptr(ws, torch.uint8, name="ws"),
@@ -632,19 +645,6 @@ def _sizes(T, B, I, V, dtype) -> Tokens:
     if (T | B | I | V) >> 31:
         raise ValueError("sizes %s must be whole numbers of 31 bits" % ((T, B, I, V),))
     return Tokens(T, B, I, V, _dt(dtype))
-
-
-def _new(shape, dtype, dev, stream):
-    """A tensor that work on `stream` (None: the current one) will use.  It is of that stream's
-    own blocks: one freed on the current stream may still be at work there.  The caller may
-    go on with it on the current stream, and free it, once that waits for `stream`."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
-    caller = torch.cuda.current_stream(dev)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=dev)
-    t.record_stream(caller)
-    return t
 
 
 def _bytes(n, what):

@@ -87,3 +87,57 @@ def check(call, made):
 @pytest.mark.parametrize("name", LANGUAGE)
 def test_language_calls(made, name):
     check(LANGUAGE[name], made)
+
+
+def layer(T=2, B=3, I=4, H=8):
+    return z(T, I, B), z(4 * H, I + H), z(64, dtype=U8), z(T, H, B)
+
+
+def bidirectional(s):
+    x, W, cache, _ = layer()
+    return L.bwd_bidir(x, x, W, W, cache, cache, z(2, 16, 3), stream=s)
+
+
+LAYERS = {
+    "fwd_cache": lambda s: L.fwd_cache(*layer()[:2], stream=s),
+    "mse_grad": lambda s: L.mse_grad(z(2, 8, 3), z(2, 8, 3), stream=s),
+    "bwd_dense": lambda s: L.bwd_dense(*layer(), stream=s),
+    "bwd_structsparse": lambda s: L.bwd_structsparse(*layer(), want_dbg=True, stream=s),
+    "bwd_stack": lambda s: L.bwd_stack(*[[a] for a in layer()[:3]], layer()[3], want_dX0=True, stream=s),
+    "bwd_bidir": bidirectional,
+    "time_reverse": lambda s: L.time_reverse(z(2, 4, 3), stream=s),
+    "bidir_join": lambda s: L.bidir_join(z(2, 8, 3), z(2, 8, 3), stream=s),
+    "select_compact": lambda s: L.select_compact(z(32, 3), stream=s),
+    "select_compact_fine": lambda s: L.select_compact(z(32, 3), kind=L.FINE, My=8, Mx=4, stream=s),
+}
+
+
+@pytest.mark.parametrize("name", LAYERS)
+def test_layer_calls(made, name):
+    check(LAYERS[name], made)
+
+
+@pytest.mark.gpu
+def test_layer_results_on_another_stream():
+    """Forward and backward of a layer on a given stream, all buffers the calls' own: the bits
+    of the current stream's calls, in memory that is not the current stream's."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    T, B, I, H = 5, 20, 40, 72
+    g = torch.Generator().manual_seed(0)
+    x, W, up = (torch.randn(s, generator=g).cuda() * 0.1 for s in ((T, I, B), (4 * H, I + H), (T, H, B)))
+
+    def calls(stream):
+        h, cache = L.fwd_cache(x, W, stream=stream)
+        return h, L.bwd_structsparse(x, W, cache, up, stream=stream)
+
+    h, want = calls(None)
+    torch.cuda.synchronize()
+    freed = torch.empty_like(h)
+    at = freed.data_ptr()
+    del freed
+    side = torch.cuda.Stream()
+    h2, got = calls(side)
+    side.synchronize()
+    assert h2.data_ptr() != at and torch.equal(h2, h)
+    assert all(torch.equal(got[k], want[k]) for k in want if want[k] is not None)
