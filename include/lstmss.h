@@ -359,7 +359,8 @@ int32_t lstmss_dropout(int64_t n, int32_t dtype, const lstmss_drop *drop, const 
 
 /* Embedding lookup: x[t][i][b] = scale * E[tokens[t][b]][i], then dropout over
  * x when drop is not NULL; formed in fp32, rounded once.
- *   E [V][I] dtype, tokens [T][B] int32, x [T][I][B] dtype (must not overlap E). */
+ *   E [V][I] dtype, tokens [T][B] int32, x [T][I][B] dtype (must not overlap E);
+ *   scale finite. */
 int32_t lstmss_embed(const lstmss_tokens *d, const void *E, const int32_t *tokens, float scale,
                      const lstmss_drop *drop, void *x, void *stream);
 

@@ -109,6 +109,9 @@ int32_t lstmss_embed(const lstmss_tokens *d, const void *E, const int32_t *token
         return rc;
     if (!E || !tokens || !x)
         return fail(LSTMSS_ERR_INVALID_ARG, "a required pointer is NULL");
+    // (the zeros of padding are scaled too)
+    if (!std::isfinite(scale))
+        return fail(LSTMSS_ERR_INVALID_ARG, "scale %g is not finite", (double)scale);
     EmbedArgs a;
     if (int32_t rc = check_drop(drop, &a.drop))
         return rc;

@@ -194,6 +194,11 @@ def test_drop_refused(L, drop, code):
     assert lib.lstmss_embed_grad(d, ANY, ANY, 1.0, p, 0, ANY, ANY, 1 << 40, NULL) == code
 
 
+@pytest.mark.parametrize("scale", [float("inf"), -float("inf"), float("nan")])
+def test_embedding_scale_refused(L, scale):
+    """A column of padding is zero: 0 times such a scale would not be."""
+    assert L.load().lstmss_embed(tokens(L), ANY, ANY, scale, NULL, ANY, NULL) == -1
+
 def test_dropout_sizes_refused(L):
     lib, p = L.load(), ctypes.byref(L.drop(0.5, 1))
     assert lib.lstmss_dropout(0, 0, p, ANY, ANY, NULL) == -1
