@@ -43,6 +43,12 @@ class LanguageConfig:
         return self.features if l == 0 else self.hidden
 
 
+def _product(a, b):
+    """a @ b in fp32, whatever the storage type: a gradient's terms are not rounded to bf16
+    before they are summed."""
+    return torch.mm(a, b) if a.dtype == torch.float32 else torch.mm(a, b, out_dtype=torch.float32)
+
+
 class LanguageModel:
     """Weights E [V][I], Ws[l] [4H][I_l + H], bs[l] [4H] (fp32), Wv [V][H]; all but the
     biases in the storage type.  step() and policy_step() train them in place."""
@@ -112,8 +118,8 @@ class LanguageModel:
         cfg, d = self.cfg, self.logits
         self.dWv.zero_()
         for t in range(cfg.steps):
-            self.dH[t] = torch.mm(self.Wv.t(), d[t])
-            self.dWv += torch.mm(d[t], self.top[t].t())
+            self.dH[t] = _product(self.Wv.t(), d[t])
+            self.dWv += _product(d[t], self.top[t].t())
         up = self.dH
         for l in range(cfg.layers - 1, -1, -1):
             if drops[l + 1] is not None:

@@ -137,6 +137,24 @@ def test_bf16_step(M):
     assert torch.isfinite(model.step(tokens, targets, sparse=True))
 
 
+def test_bf16_vocabulary_products_are_summed_in_fp32(M):
+    """The vocabulary's gradient and the top layer's, from the gradient in the logits and the
+    activations as they are stored.  A product of two bf16 numbers is exact in fp32, so only the
+    additions round: within 2^-23 of the terms' sizes each, in any order, by either rounding."""
+    T, B, V = 5, 4, 40
+    cfg = M.LanguageConfig(vocabulary=V, features=16, hidden=24, layers=1, batch=B, steps=T, dropout=0.0,
+                           dtype=torch.bfloat16)
+    model = M.LanguageModel(cfg, *M.make_weights(cfg))
+    model.step(*M.synthetic_batch(cfg, 8), update=False)
+    d, top, Wv = (t.double().cpu() for t in (model.logits, model.top, model.Wv))
+    want = sum(d[t] @ top[t].t() for t in range(T))
+    size = sum(d[t].abs() @ top[t].t().abs() for t in range(T))
+    assert ((model.dWv.double().cpu() - want).abs() <= (B + T) * 2.0**-23 * size + 2.0**-126).all()
+    for t in range(T):
+        size = Wv.t().abs() @ d[t].abs()
+        assert ((model.dH[t].double().cpu() - Wv.t() @ d[t]).abs() <= V * 2.0**-23 * size + 2.0**-126).all()
+
+
 def test_shapes_refused(M):
     cfg = M.LanguageConfig(vocabulary=20, features=8, hidden=16, layers=1, batch=2, steps=2)
     E, Ws, bs, Wv = M.make_weights(cfg)
