@@ -451,6 +451,7 @@ def test_gradients_at_any_offset(L, dtype, T, V, B):
     slope = 0.25 * w * (np.abs(adv) * np.exp(0.07) + 0.125 * np.exp(0.31))
     check_grad(L, out["dlogits"], x, d, g, V, dtype, tol, slope * tol + 4 * U * np.abs(g))
 
+
 def test_xent_against_differences(L):
     """Central differences of the loss along one direction: h^2 / 6 of its third derivative and
     the loss's rounding over h."""
@@ -647,6 +648,7 @@ def test_new_tensors_of_a_call_on_another_stream(L):
     assert y.data_ptr() != at and torch.equal(y, ref)
     again = torch.empty_like(x)
     assert again.data_ptr() == at          # it is still the current stream's
+
 
 def test_calls_in_a_captured_graph(L):
     """Recorded by the caller and replayed, with eager work between: every replay gives the

@@ -199,6 +199,7 @@ def test_embedding_scale_refused(L, scale):
     """A column of padding is zero: 0 times such a scale would not be."""
     assert L.load().lstmss_embed(tokens(L), ANY, ANY, scale, NULL, ANY, NULL) == -1
 
+
 def test_dropout_sizes_refused(L):
     lib, p = L.load(), ctypes.byref(L.drop(0.5, 1))
     assert lib.lstmss_dropout(0, 0, p, ANY, ANY, NULL) == -1
