@@ -344,7 +344,8 @@ typedef struct {
  *   offset  a multiple of 8: what earlier calls with this seed have taken,
  *           each rounded up to a multiple of 8
  *   period  0, or the length after which the mask repeats, >= 1: H * B on
- *           [T][H][B] is one mask for all steps */
+ *           [T][H][B] is one mask for all steps (a multiple of 8 is two to four
+ *           times faster than another length) */
 typedef struct {
     float p;
     uint64_t seed, offset;
@@ -366,7 +367,9 @@ int32_t lstmss_embed(const lstmss_tokens *d, const void *E, const int32_t *token
 
 /* Its gradient: dE[v][i] = scale * the sum of dropout(dX)[t][i][b] over the
  * (t, b) with token v, in fp32, in an order that the tokens alone decide (the
- * tokens are sorted, equal ones by position: no atomics).
+ * tokens are sorted, equal ones by position: no atomics).  The sort's time
+ * grows with T * B * V: 1.2 ms where that is 2^40, by which rate the largest
+ * sizes taken need some 20 s.
  *   dX [T][I][B] fp32, dE [V][I] fp32; drop as given to lstmss_embed, or NULL
  *   accumulate  0: dE is overwritten (rows of absent tokens with zero);
  *               1: the sums are added to it (rows of absent tokens are not
@@ -394,7 +397,8 @@ int32_t lstmss_embed_grad(const lstmss_tokens *d, const int32_t *tokens, const f
  * [T][B] fp32 or NULL (lstmss_token_logp: required), dlogits [T][V][B] dtype
  * or NULL = dL/dlogits; dlogits may be logits itself.  Where r * adv equals the
  * clipped product the gradient is the unclipped one's.
- * The softmax's sum is of fp32, per-token terms are of fp64.
+ * The softmax's sum is of fp32, per-token terms are of fp64; what is common to
+ * a column's logits takes no part, however large.
  *   ws  lstmss_loss_workspace_bytes(d) bytes. */
 typedef struct {
     float clip_low, clip_high; /* >= 0, clip_low <= 1 */

@@ -5,9 +5,12 @@
 // in one piece, x its batch: a work-group reads 64 features of up to 64
 // columns' rows, turns them over in LDS and writes them batch-last.  Bound by
 // the memory (the rows in use read, x written), with dropout on bf16 also by
-// Philox.  100 x 256 tokens of a Zipf law, 4096 features, 32000 rows: bf16 44 us,
-// with dropout 55 to 61 (210 MB written, about 60 MB of rows: 4.8 TB/s); fp32 86
-// and 89.
+// Philox.  100 x 256 tokens of a Zipf law, 4096 features, 32000 rows, three sets
+// of tokens in turn: bf16 57 us (210 MB written, about 60 MB of rows: 4.8 TB/s),
+// with dropout 68; fp32 132 and 142.  The same tokens again, whose rows are then in
+// the last-level cache: 44, 57; 84, 90.  A batch that is no multiple of 64 takes
+// the kernel's general form: 100 x 255 tokens, 4095 features, bf16 with dropout
+// 191 us, and 407 with a mask that repeats after no multiple of 8.
 //
 // Gradient: dE[v][i] = scale * sum of dX[t][i][b] over the (t, b) with token v.
 //   sort_kernel   the positions' ranks by (token, position), and each token's
@@ -20,9 +23,10 @@
 //   carry_kernel  tokens whose rows lie in several groups
 // (few positions: sort_kernel and few_kernel alone).  The order of every sum
 // follows from the tokens alone.  Bound by the memory: 50 x 128 tokens, 2048
-// features, 32000 rows 85 us (dE 262 MB written, dX 52 MB read: 3.7 TB/s; the
-// sort with the zeroing 36 to 49 us, the turn 21, the walk 9, the carry 5);
-// 35 x 20 tokens, 650 features, 10000 rows 12 us, two launches of 6.5.
+// features, 32000 rows 83 us (dE 262 MB written, dX 52 MB read: 3.8 TB/s; the
+// sort with the zeroing 48 us, the turn 21, the walk 9, the carry 5), added to dE
+// 49 (10, 24, 11, 4); 35 x 20 tokens, 650 features, 10000 rows 12 us, two launches
+// of 7 and 6.  The sort is what grows with N * V: see there.
 #include <algorithm>
 
 #include "common.h"
@@ -134,7 +138,8 @@ __device__ __forceinline__ void write_tile(const EmbedArgs &a, const Tiling &g, 
 
 // A work-group's columns and `run` feature tiles one after the other: the next
 // tile's rows are on their way while this one is turned over and written
-// (4096 bf16 features, us: 79 and, with dropout, 92 so, 85 and 107 without).
+// (4096 bf16 features, us: 79 and, with dropout, 92 so, 85 and 107 without; x was
+// not streamed then).
 // WHOLE: B is a multiple of 64, and the mask repeats after a multiple of 8 if
 // at all; DROP: with dropout (only told apart there).  PAST: x is streamed.
 template <typename TS, bool WHOLE, bool DROP, bool PAST>
@@ -216,10 +221,15 @@ __device__ __forceinline__ void zero_fill(float *p, long i0, long i1) {
 // of the positions by token; the counts before a (wave, token), with those of
 // all smaller tokens, are where that wave's first position of the token goes,
 // and the waves then go over their shares again in order.  Every work-group
-// reads all tokens, which lie in the caches; none waits for another.  Bound by
-// latency: 7 us for 700 tokens, and hidden by the zeroing for more.
+// reads all tokens twice, which lie in the caches; none waits for another.  So a
+// small call is bound by latency, and the time of a large one grows with N * V / R:
+// without zeroing 5 us for 700 tokens of 10000 rows, 10 for 6400 of 32000, 45 for
+// 25600 of 1000000, 1225 for 2^20 of 2^20 (the call's other kernels: 240, for 64
+// features).
 // The work-groups from `sorters` on zero dE meanwhile, which the sort leaves
-// the memory free for: rows in use are written after this launch.
+// the memory free for: rows in use are written after this launch.  That hides
+// the sort where dE is what takes longer (6400 tokens, 262 MB: 48 us), not where
+// N * V is (25600 tokens, 32 MB: 48).
 __global__ __launch_bounds__(SORT_NT) void sort_kernel(const int32_t *tokens, int N, int V, int R, int32_t *rank,
                                                        int32_t *order, int32_t *key, int32_t *start, int sorters,
                                                        float *dE, long size) {

@@ -50,7 +50,9 @@ __device__ __forceinline__ void drop_whole(const DropArgs &d, long e, float *f) 
         f[k] = (k & 1 ? w[k >> 1] : w[k >> 1] << 16) >= thr ? f[k] * d.scale : 0.f;
 }
 
-// The same for any mask.
+// The same for any mask.  One that repeats after no multiple of 8 takes a
+// generator and a 64-bit remainder for each element: four times the time of a
+// dropout over bf16, twice that of one over fp32.
 template <int VEC>
 __device__ __forceinline__ void drop_any(const DropArgs &d, long e, float *f) {
     if (d.thr == 0)

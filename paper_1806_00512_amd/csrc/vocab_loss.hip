@@ -17,8 +17,8 @@
 //
 // Bound by the memory, which gives the logits twice and takes the gradient
 // once.  Loss and gradient of 50 x 32000 x 128 logits (us): bf16 199 (1.23 GB, 6.2
-// TB/s; sums 72 to 80, tokens 5, gradient 120 to 125), fp32 370 (6.6 TB/s);
-// 35 x 10000 x 20 fp32 22.5 (sums 8, tokens 3, gradient 9).  Joining the token's
+// TB/s; sums 78, tokens 5, gradient 123), fp32 381 (6.4 TB/s; 128, 6, 252);
+// 35 x 10000 x 20 fp32 22.8 (9, 4, 11).  Joining the token's
 // terms to the gradient's work-groups, which saves a launch, measured slower
 // (23 to 48 us against 22 to 32): fp64 logarithms and exponentials of all tokens
 // then wait for one work-group.
@@ -41,6 +41,12 @@ constexpr int NT = 256; // threads of a work-group at most
 // value seen or up to GROW below the largest one.  Empty: the lowest finite
 // number and 0, which needs no case of its own: a column of -inf alone ends
 // with s = 0.
+//
+// Exponentials are the hardware's 2^z of the product with log2 e, within (|x - m|
+// + 1) 2^-23 of themselves: the sum's small terms have the large errors, and an
+// element of the gradient keeps its own in proportion (what is below 2^-126 may
+// come out as zero).  An accurate one takes several instructions more, for which
+// bf16 logits leave no room.
 struct Stat {
     float m, s;
 };
@@ -159,7 +165,8 @@ __device__ __forceinline__ void load_edge(const TS *x, long at, long lo, long hi
 }
 
 // (m, s) of a chunk's columns.  Bound by the memory and, in bf16, nearly by the
-// exponentials: 410 MB in 72 us past the caches, where reading alone takes 58.
+// exponentials: 410 MB in 78 us, most of it past the caches, where reading alone
+// takes 58.
 template <typename TS>
 __global__ __launch_bounds__(NT) void stat_flat_kernel(Cut g, const TS *logits, Stat *stat) {
     constexpr int U = 4, VEC = vec_of<TS>();
@@ -222,8 +229,9 @@ __global__ __launch_bounds__(NT) void stat_flat_kernel(Cut g, const TS *logits, 
 }
 
 // The same for rows wider than a work-group's vectors, as of one product for all
-// steps: 1 x 32000 x 6400 bf16 70 us with the token kernel (5.8 TB/s), 1 x 32000 x
-// 6399, whose vectors straddle lines, 123.
+// steps: 1 x 32000 x 6400 bf16 85 us (4.8 TB/s), 1 x 32000 x 6399, whose vectors
+// straddle lines, 139 (with the token kernel, on the same logits again: 73 and 123).
+// Their gradients take 135 and 160.
 template <typename TS>
 __global__ __launch_bounds__(NT) void stat_wide_kernel(Cut g, const TS *logits, Stat *stat) {
     constexpr int U = 4, VEC = vec_of<TS>();
@@ -348,7 +356,7 @@ __device__ __forceinline__ double token_terms(const LossArgs &a, Stat q, const T
 
 // 16 tokens to a work-group, 16 threads to a token: they join its chunks, and
 // one of them does its terms in fp64, on operands read while the chunks were.
-// Bound by latency: 3 us for 700 tokens, 5 for 6400.
+// Bound by latency: 4 us for 700 tokens, 5 for 6400.
 constexpr int TOKENS = 16;
 
 __global__ __launch_bounds__(NT) void token_kernel(LossArgs a, int chunks, const Stat *stat, Coef *coef, float *dtarget,
@@ -391,7 +399,7 @@ __global__ __launch_bounds__(NT) void token_kernel(LossArgs a, int chunks, const
 // Sums and terms in one launch, for small logits: a work-group takes VEC columns
 // of a step through all its rows.  The work-groups of a step read the same
 // lines, so they go to one XCD (every eighth) while there are eight steps.
-// Bound by latency, 5 to 6 us.
+// Bound by latency: 1 x 10000 x 16 fp32 8.5 us.
 constexpr int NARROW_NT = 1024;
 
 template <typename TS>
@@ -509,7 +517,7 @@ __device__ __forceinline__ void grad_targets(const Cut &g, const Piece &p, int b
 }
 
 // The gradient of a piece.  Bound by the memory: 410 MB of bf16 logits, about
-// half of them from the last-level cache, and 410 MB of gradient in 120 us (6.8
+// half of them from the last-level cache, and 410 MB of gradient in 123 us (6.7
 // TB/s).  PAST: it is streamed.
 template <typename TS, bool PAST>
 __global__ __launch_bounds__(NT) void grad_flat_kernel(Cut g, const TS *logits, TS *dlogits, const int32_t *targets,
@@ -640,8 +648,8 @@ long stat_groups(int T, int B, int V, int es) {
 
 // What of the logits the first kernel leaves in the last-level cache (256 MB)
 // for the gradient: the last of them; what comes before is read past it, which
-// is faster by a fifth. 50 x 32000 x 128 bf16 (410 MB), loss and gradient: 224 us;
-// all of it through the cache 233, all past it 238.
+// is faster by a fifth. 50 x 32000 x 128 bf16 (410 MB), loss and gradient, in pieces
+// of about 25 KB: 224 us; all of it through the cache 233, all past it 238.
 constexpr long KEEP_BYTES = 224L << 20;
 
 // The cut of logits whose elements have es bytes.
