@@ -512,7 +512,7 @@ int32_t lstmss_muon_update(const lstmss_orth *d, const lstmss_muon *p, const voi
  *   score = scores[n] + logits[v][n] - log sum exp(logits[:][n]),
  * the K largest above -inf, in falling order, ties to the lowest k * V + v; the
  * j-th goes to column s * K + j of the outputs.  Comparisons are of scores in
- * 64 bits, their softmax's sum of fp32 exponentials.
+ * 64 bits; their log sum exp is of fp32 exponentials, within (25 + 2.3 ln V) 2^-24.
  *   logits [V][N] dtype: -inf bars a token, NaN does too, +inf counts as the
  *     largest finite number; a column without any other has no candidates
  *   scores [N] fp32: -inf (or NaN) for a beam that is not there; the first

@@ -52,9 +52,20 @@ struct Scan {
 };
 
 // A wavefront: a group of tokens, cx vectors of columns; 64 / cx lanes share a
-// vector's rows, 8 of which are on their way at once.  32000 x 512 bf16 logits 14 to
-// 16 us (7 us is their reading), 10000 x 4 in fp32 5.5 us: loads, then exponentials,
-// then six exchanges between lanes, with little to overlap.
+// vector's rows, 8 of which are on their way at once.
+//
+// Exponentials are the hardware's, of fp32 differences from a reference of the
+// lane's own that moves only when a logit is 8 above it; eight of them are added
+// in fp32 and the eights in 64 bits, since terms of one size added to a large
+// fp32 sum are rounded the same way each time (2^22 tokens, 32 beams: the sum's
+// logarithm was off by 202 u, u = 2^-24).  Whatever V is, it is within u (25 + 2.3 d),
+// d the distance below the largest logit, averaged by the softmax and at most ln
+// V: a term's exponential 2 + 2.3 d, eight terms' sum 7, moves of the reference 4 (two
+// of them leave nothing of 2^18 terms), the lane's factor 2 and two roundings, the
+// lanes' sum 6, the group's factor 2 and a rounding.
+//
+// 32000 x 512 bf16 logits 14 to 16 us (7 us is their reading), 10000 x 4 in fp32 5.5 us:
+// loads, then exponentials, then exchanges between lanes, with little to overlap.
 template <typename TS>
 __global__ void __launch_bounds__(256) beam_scan_kernel(const Scan a, const TS *x) {
     constexpr int VEC = vec_of<TS>(), AHEAD = 8;
@@ -65,11 +76,12 @@ __global__ void __launch_bounds__(256) beam_scan_kernel(const Scan a, const TS *
     const int col = ((wave - group * a.tiles) * a.cx + c) * VEC;
     const int n = min(VEC, a.N - col); // columns that are there (0 or less: none)
     const int v0 = group * a.rows, v1 = min(a.V, v0 + a.rows);
-    float m[VEC], s[VEC];
+    float m[VEC], ref[VEC]; // largest, reference of the sum
+    double s[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-        m[k] = -INFINITY;
-        s[k] = 0.f;
+        m[k] = ref[k] = -INFINITY;
+        s[k] = 0.0;
     }
     if (n > 0)
         for (int v = v0 + lane / a.cx; v < v1; v += AHEAD * rl) {
@@ -95,29 +107,37 @@ __global__ void __launch_bounds__(256) beam_scan_kernel(const Scan a, const TS *
                     f[i][k] = clean(f[i][k]);
                     top = fmaxf(top, f[i][k]);
                 }
+                m[k] = top;
+                if (top > ref[k] + 8.f) {
+                    s[k] *= exp_of(ref[k] - top);
+                    ref[k] = top;
+                }
                 if (top > -INFINITY) {
-                    float add = s[k] * exp_of(m[k] - top);
+                    float add = 0.f;
 #pragma unroll
                     for (int i = 0; i < AHEAD; ++i)
-                        add += exp_of(f[i][k] - top);
-                    s[k] = add;
-                    m[k] = top;
+                        add += exp_of(f[i][k] - ref[k]);
+                    s[k] += add;
                 }
             }
         }
+    float sum[VEC];
     for (int d = a.cx; d < 64; d *= 2)
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-            const float om = shfl_xor_f32(m[k], d), os = shfl_xor_f32(s[k], d), top = fmaxf(m[k], om);
-            if (top > -INFINITY)
-                s[k] = s[k] * exp_of(m[k] - top) + os * exp_of(om - top);
-            m[k] = top;
-        }
+        for (int k = 0; k < VEC; ++k)
+            m[k] = fmaxf(m[k], shfl_xor_f32(m[k], d));
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+        sum[k] = ref[k] > -INFINITY ? (float)(s[k] * exp_of(ref[k] - m[k])) : 0.f;
+    for (int d = a.cx; d < 64; d *= 2)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+            sum[k] += shfl_xor_f32(sum[k], d);
     if (lane < a.cx)
 #pragma unroll
         for (int k = 0; k < VEC; ++k)
             if (k < n)
-                a.groups_of[(long)group * a.N + col + k] = float2{m[k], s[k]};
+                a.groups_of[(long)group * a.N + col + k] = float2{m[k], sum[k]};
 }
 
 struct Pick {

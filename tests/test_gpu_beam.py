@@ -365,3 +365,42 @@ def test_steps_on_two_streams_at_once(L):
     torch.cuda.synchronize()
     for o, (_, _, _, want, _) in zip(got, ins):
         assert all(torch.equal(o[k], want[k]) for k in want)
+
+
+@pytest.mark.parametrize("dtype,V", [("f32", 1 << 18), ("f32", 1 << 20), ("bf16", 1 << 22)])
+def test_sums_of_many_tokens_keep_their_order(L, dtype, V):
+    """32 beams over many tokens, so that a group has 2^10 to 2^14 of them: one token 3, of the
+    others of a column 64 in 1024 0 and the rest the same (terms whose rounded sums err in one
+    direction), or all slowly rising.  The beams' best candidates are 1e-5 apart and come out in
+    their order.
+
+    In units of u = 2^-24 a term's exponential is within 2 (the instruction) + 2.3 d (the
+    difference, the constant and their product), d the distances to the references on its way;
+    eight terms' sum adds 7, the lane's factor 2 and two roundings, the lanes' sum 6, the group's
+    factor 2 and a rounding: 21 u + 2.3 u times the softmax's mean of d.  A reference is the
+    largest logit or below it by no more than the rise, which d counts twice then."""
+    K, u = 32, 2.0**-24
+    g = torch.Generator(device=DEV)
+    g.manual_seed(23)
+    logits = torch.empty(V, K, dtype=TYPES[dtype], device=DEV)
+    v = torch.arange(V, device=DEV, dtype=torch.float64)
+    for k in range(K):
+        logits[:, k] = v / V - 1.0 if k % 4 == 3 else torch.where(v % 1024 < 64, 0.0, (-1.1, -9.0, -5.3)[k % 4])
+        logits[int(torch.randint(0, V, (1,), generator=g, device=DEV)), k] = 3.0
+    lse, bound = np.empty(K), np.empty(K)
+    for k in range(K):
+        x = logits[:, k].double().cpu().numpy()
+        e = np.exp(x - 3.0)
+        lse[k] = 3.0 + np.log(e.sum())
+        bound[k] = u * (21 + 2.3 * ((e * (3.0 - x)).sum() / e.sum() + (2.0 if k % 4 == 3 else 0.0)))
+    place = np.array([7 * k % K for k in range(K)])
+    scores = torch.from_numpy(lse - 3.0 - 1e-5 * place).float().to(DEV)
+    want = scores.cpu().numpy().astype(np.float64) + (3.0 - lse)
+    order = np.argsort(-want)
+    gaps = want[order][:-1] - want[order][1:]
+    assert (gaps > bound[order][:-1] + bound[order][1:]).all()
+    o = L.beam_step(logits, scores, K)
+    assert o["parents"].tolist() == order.tolist()
+    assert o["tokens"].tolist() == logits.argmax(0)[torch.from_numpy(order).to(DEV)].tolist()
+    err = np.abs(o["scores"].cpu().numpy().astype(np.float64) - want[order])
+    assert (err <= bound[order] + u * np.abs(want[order])).all(), (err / u).max()
