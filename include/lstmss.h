@@ -419,7 +419,9 @@ int32_t lstmss_policy_loss(const lstmss_tokens *d, const lstmss_policy *p, const
 
 /* The head of a language model: the layer between the stack's top and the
  * tokens, the update of its and the layers' weights, and the search that
- * answers from the logits.
+ * answers from the logits.  Outputs and workspaces that overlap an input or each
+ * other are refused (LSTMSS_ERR_INVALID_ARG), but for an output that is, whole,
+ * the input named with it.
  *
  * Linear layer on batch-last tensors:
  *   z[t][n][b] = sum over k of W[n][k] x[t][k][b] + b[n],  y = act(z) + res
@@ -432,7 +434,6 @@ int32_t lstmss_policy_loss(const lstmss_tokens *d, const lstmss_policy *p, const
  *   dtype or NULL (may be y); z [T][N][B] dtype or NULL: receives the
  *   pre-activation that the gradient needs (neither y nor res)
  *   ws  lstmss_linear_workspace_bytes(d) bytes (may be 0, with ws NULL)
- * y and z must not overlap x, W or b.
  *
  * Its gradients, with g = dY * act'(z) formed in fp32 (relu'(0) = 0):
  *   dX[t][k][b] = sum over n of W[n][k] g[t][n][b]
@@ -441,8 +442,7 @@ int32_t lstmss_policy_loss(const lstmss_tokens *d, const lstmss_policy *p, const
  *   x, W as above (x may be NULL without dW, W without dX); z as
  *   lstmss_linear stored it, NULL where act is none; dY [T][N][B] of dy_dtype
  *   dX [T][K][B], dW [N][K], db [N] fp32, each may be NULL
- *   accumulate  0: dW and db are overwritten; 1: added to (dX is overwritten);
- *   they must not overlap the inputs
+ *   accumulate  0: dW and db are overwritten; 1: added to (dX is overwritten)
  *   ws  lstmss_linear_grad_workspace_bytes(d, dy_dtype) bytes.
  * Sums are taken in an order that the sizes alone decide.
  * Sizes: T * B, K and N at most 2^20; T * B * K, T * B * N and N * K below 2^32. */

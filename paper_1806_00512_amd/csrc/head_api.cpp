@@ -8,6 +8,34 @@
 
 namespace {
 
+// Memory of an argument (at NULL: none).
+struct Span {
+    const void *at;
+    int64_t bytes;
+};
+
+// Outputs that share memory with an input or with another output.
+bool meets(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
+    auto shared = [](const Span &a, const Span &b) {
+        const uintptr_t p = (uintptr_t)a.at, q = (uintptr_t)b.at;
+        return p && q && a.bytes > 0 && b.bytes > 0 && (p < q ? q - p < (uintptr_t)a.bytes : p - q < (uintptr_t)b.bytes);
+    };
+    for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+        for (const Span &i : inputs)
+            if (shared(*o, i))
+                return true;
+        for (auto p = outputs.begin(); p != o; ++p)
+            if (shared(*o, *p))
+                return true;
+    }
+    return false;
+}
+
+// An input that may be the output `out` itself, but not share a part of it.
+Span or_out(const void *in, const void *out, int64_t bytes) { return {in == out ? nullptr : in, bytes}; }
+
+int64_t size_of(int32_t dtype) { return dtype == LSTMSS_BF16 ? 2 : 4; }
+
 int32_t check_linear(const lstmss_linear_dims *d) {
     if (!d)
         return fail(LSTMSS_ERR_INVALID_ARG, "sizes are NULL");
@@ -57,8 +85,15 @@ int32_t muon_call(const char *what, const lstmss_orth *d, MuonArgs &a, void *ws,
     a.b = d->b;
     a.c = d->c;
     a.eps = 1e-7f;
-    if (int32_t rc = check_ws(ws, ws_bytes, muon_ws(a.R, a.C, a.blocks)))
+    const size_t need = muon_ws(a.R, a.C, a.blocks);
+    if (int32_t rc = check_ws(ws, ws_bytes, need))
         return rc;
+    const int64_t n = (int64_t)a.blocks * a.R * a.C, es = size_of(d->dtype);
+    if (a.W ? meets({{a.Wo, n * es}, {a.Mo, n * 4}, {ws, (int64_t)need}},
+                    {or_out(a.W, a.Wo, n * es), or_out(a.M, a.Mo, n * 4), {a.dW, n * 4}})
+            : meets({{a.Wo, n * es}, {ws, (int64_t)need}}, {or_out(a.dW, a.Wo, n * es)}))
+        return fail(LSTMSS_ERR_INVALID_ARG,
+                    "an output may be its input (W_out W, M_out M, X_out G), but must overlap nothing else");
     a.ws = ws;
     return enqueue(what, stream, [&] { return launch_muon(a, (hipStream_t)stream); });
 }
@@ -85,21 +120,6 @@ int32_t check_columns(int64_t N, int32_t K) {
     return LSTMSS_OK;
 }
 
-// Outputs that are an input, or another output (NULL is neither).
-bool meets(std::initializer_list<const void *> outputs, std::initializer_list<const void *> inputs) {
-    for (auto o = outputs.begin(); o != outputs.end(); ++o) {
-        if (!*o)
-            continue;
-        for (const void *i : inputs)
-            if (*o == i)
-                return true;
-        for (auto p = outputs.begin(); p != o; ++p)
-            if (*o == *p)
-                return true;
-    }
-    return false;
-}
-
 int32_t check_some_ws(const void *ws, size_t have, size_t need) {
     return need ? check_ws(ws, have, need) : LSTMSS_OK;
 }
@@ -120,8 +140,6 @@ int32_t lstmss_linear(const lstmss_linear_dims *d, const void *x, const void *W,
         return rc;
     if (!x || !W || !y)
         return fail(LSTMSS_ERR_INVALID_ARG, "a required pointer is NULL");
-    if (meets({y, z}, {x, W, b}) || (z && z == res))
-        return fail(LSTMSS_ERR_INVALID_ARG, "y and z must be no input (y may be res) and not each other");
     LinearArgs a;
     a.T = d->T;
     a.B = d->B;
@@ -129,8 +147,13 @@ int32_t lstmss_linear(const lstmss_linear_dims *d, const void *x, const void *W,
     a.N = d->N;
     a.act = d->act;
     a.bf16 = d->dtype == LSTMSS_BF16;
-    if (int32_t rc = check_some_ws(ws, ws_bytes, linear_ws(a.T, a.B, a.K, a.N, a.bf16)))
+    const size_t need = linear_ws(a.T, a.B, a.K, a.N, a.bf16);
+    if (int32_t rc = check_some_ws(ws, ws_bytes, need))
         return rc;
+    const int64_t es = size_of(d->dtype), J = (int64_t)a.T * a.B, out = J * a.N * es;
+    if (meets({{y, out}, {z, out}, {ws, (int64_t)need}},
+              {{x, J * a.K * es}, {W, (int64_t)a.N * a.K * es}, {b, a.N * 4l}, or_out(res, y, out)}))
+        return fail(LSTMSS_ERR_INVALID_ARG, "y, z and ws must overlap no input (y may be res) and not each other");
     a.x = x;
     a.W = W;
     a.b = b;
@@ -161,8 +184,6 @@ int32_t lstmss_linear_grad(const lstmss_linear_dims *d, const void *x, const voi
         return fail(LSTMSS_ERR_INVALID_ARG, "a required pointer is NULL");
     if ((d->act != LSTMSS_ACT_NONE) != (z != nullptr))
         return fail(LSTMSS_ERR_INVALID_ARG, "z is needed where there is an activation, and only there");
-    if (meets({dX, dW, db}, {x, W, z, dY}))
-        return fail(LSTMSS_ERR_INVALID_ARG, "a gradient must be no input and no other gradient");
     LinearGradArgs a;
     a.T = d->T;
     a.B = d->B;
@@ -171,9 +192,13 @@ int32_t lstmss_linear_grad(const lstmss_linear_dims *d, const void *x, const voi
     a.act = d->act;
     a.bf16 = d->dtype == LSTMSS_BF16;
     a.dy_bf16 = dy_dtype == LSTMSS_BF16;
-    if (int32_t rc = check_some_ws(ws, ws_bytes,
-                                   linear_grad_ws(a.T, a.B, a.K, a.N, a.bf16, a.dy_bf16, a.act)))
+    const size_t need = linear_grad_ws(a.T, a.B, a.K, a.N, a.bf16, a.dy_bf16, a.act);
+    if (int32_t rc = check_some_ws(ws, ws_bytes, need))
         return rc;
+    const int64_t es = size_of(d->dtype), J = (int64_t)a.T * a.B, NK = (int64_t)a.N * a.K;
+    if (meets({{dX, J * a.K * 4}, {dW, NK * 4}, {db, a.N * 4l}, {ws, (int64_t)need}},
+              {{x, J * a.K * es}, {W, NK * es}, {z, J * a.N * es}, {dY, J * a.N * size_of(dy_dtype)}}))
+        return fail(LSTMSS_ERR_INVALID_ARG, "gradients and ws must overlap no input and not each other");
     a.x = x;
     a.W = W;
     a.z = z;
@@ -218,8 +243,6 @@ int32_t lstmss_muon_update(const lstmss_orth *d, const lstmss_muon *p, const voi
                     (double)p->decay, (double)p->scale);
     if (!(p->momentum >= 0.f) || !(p->momentum < 1.f))
         return fail(LSTMSS_ERR_INVALID_ARG, "momentum=%g must be in [0, 1)", (double)p->momentum);
-    if (meets({W_out, M_out}, {dW}) || (const void *)W_out == (const void *)M || (const void *)M_out == W)
-        return fail(LSTMSS_ERR_INVALID_ARG, "W_out may be W and M_out M, but no other input");
     MuonArgs a = {};
     a.lr = p->lr;
     a.mu = p->momentum;
@@ -251,12 +274,14 @@ int32_t lstmss_beam_step(const lstmss_beams *d, const void *logits, const float 
         return fail(LSTMSS_ERR_INVALID_ARG, "eos=%d must be -1 or in [0, %d)", eos, d->V);
     if (eos < 0 && (done || done_out))
         return fail(LSTMSS_ERR_INVALID_ARG, "no beam is finished without an eos");
-    if (meets({scores_out, tokens, parents, done_out}, {logits}) || meets({tokens, parents}, {scores, done}) ||
-        (const void *)scores_out == (const void *)done || (const void *)done_out == (const void *)scores)
-        return fail(LSTMSS_ERR_INVALID_ARG,
-                    "scores_out may be scores and done_out done, but no other input or output");
-    if (int32_t rc = check_ws(ws, ws_bytes, beam_ws(d->S, d->K, d->V)))
+    const size_t need = beam_ws(d->S, d->K, d->V);
+    if (int32_t rc = check_ws(ws, ws_bytes, need))
         return rc;
+    const int64_t N = (int64_t)d->S * d->K, n = N * 4;
+    if (meets({{scores_out, n}, {tokens, n}, {parents, n}, {done_out, n}, {ws, (int64_t)need}},
+              {{logits, d->V * N * size_of(d->dtype)}, or_out(scores, scores_out, n), or_out(done, done_out, n)}))
+        return fail(LSTMSS_ERR_INVALID_ARG,
+                    "scores_out may be scores and done_out done, but outputs must overlap nothing else");
     BeamArgs a;
     a.S = d->S;
     a.K = d->K;
@@ -286,8 +311,9 @@ int32_t lstmss_beam_reorder(int64_t rows, int32_t N, int32_t K, int32_t dtype, c
         return fail(LSTMSS_ERR_UNSUPPORTED, "unknown dtype %d", dtype);
     if (!parents || !x || !out)
         return fail(LSTMSS_ERR_INVALID_ARG, "a required pointer is NULL");
-    if (x == out)
-        return fail(LSTMSS_ERR_INVALID_ARG, "out must not be x");
+    const int64_t bytes = rows * N * size_of(dtype);
+    if (meets({{out, bytes}}, {{x, bytes}, {parents, N * 4l}}))
+        return fail(LSTMSS_ERR_INVALID_ARG, "out must overlap neither x nor parents");
     return enqueue("beam_reorder", stream, [&] {
         return launch_beam_reorder((long)rows, N, K, dtype == LSTMSS_BF16, parents, x, out, (hipStream_t)stream);
     });
@@ -301,8 +327,9 @@ int32_t lstmss_beam_trace(int32_t T, int32_t N, int32_t K, const int32_t *tokens
         return fail(LSTMSS_ERR_INVALID_ARG, "T=%d must be positive", T);
     if (!tokens || !parents || !out)
         return fail(LSTMSS_ERR_INVALID_ARG, "a required pointer is NULL");
-    if (out == tokens || out == parents)
-        return fail(LSTMSS_ERR_INVALID_ARG, "out must be neither tokens nor parents");
+    const int64_t bytes = (int64_t)T * N * 4;
+    if (meets({{out, bytes}}, {{tokens, bytes}, {parents, bytes}}))
+        return fail(LSTMSS_ERR_INVALID_ARG, "out must overlap neither tokens nor parents");
     return enqueue("beam_trace", stream,
                    [&] { return launch_beam_trace(T, N, K, tokens, parents, out, (hipStream_t)stream); });
 }

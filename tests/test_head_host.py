@@ -180,3 +180,75 @@ def test_beam_arguments_refused(lib):
     assert trace(T=0) == INVALID and trace(N=13) == INVALID and trace(out=P) == INVALID
     for name in ("t", "p", "out"):
         assert trace(**{name: None}) == INVALID
+
+
+def places(count):
+    """Addresses far from each other."""
+    return [(4 + i) << 30 for i in range(count)]
+
+
+def refuses(call, names, sizes, outputs):
+    """Every output, and the workspace, that shares its last or first element with another
+    argument: sizes[name] bytes of elements of two bytes or more."""
+    at = dict(zip(names, places(len(names))))
+    for o in outputs + ["ws"] * ("ws" in names):
+        for other in names:
+            if o == other:
+                continue
+            a, b = (other, o) if o == "ws" else (o, other)  # (the workspace keeps its alignment)
+            for p in (at[b] - sizes[a] + 2, at[b] + sizes[b] - 2):
+                assert call(**{**at, a: p}) == INVALID, (a, b)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_linear_refuses_memory_that_overlaps(lib, dtype):
+    T, B, K, N = 3, 50, 20, 30
+    d, es = L.LinearDims(T, B, K, N, dtype, 4), (4, 2)[dtype]
+    need = lib.lstmss_linear_workspace_bytes(ref(d))
+    names = ["x", "W", "b", "res", "z", "y", "ws"]
+    sizes = dict(x=T * K * B * es, W=N * K * es, b=4 * N, res=T * N * B * es, z=T * N * B * es, y=T * N * B * es, ws=need)
+    call = lambda x, W, b, res, z, y, ws: lib.lstmss_linear(ref(d), x, W, b, res, z, y, ws, need, None)  # noqa: E731
+    refuses(call, names, sizes, ["y", "z"])
+    need = lib.lstmss_linear_grad_workspace_bytes(ref(d), 0)
+    names = ["x", "W", "z", "dY", "dX", "dW", "db", "ws"]
+    sizes = dict(x=T * K * B * es, W=N * K * es, z=T * N * B * es, dY=T * N * B * 4, dX=T * K * B * 4, dW=N * K * 4,
+                 db=4 * N, ws=need)
+    grad = lambda x, W, z, dY, dX, dW, db, ws: lib.lstmss_linear_grad(  # noqa: E731
+        ref(d), x, W, z, dY, 0, 0, dX, dW, db, ws, need, None)
+    refuses(grad, names, sizes, ["dX", "dW", "db"])
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_muon_refuses_memory_that_overlaps(lib, dtype):
+    d, p, n = L.Orth(40, 60, 2, dtype, 5, *L.NEWTON_SCHULZ), L.Muon(0.1, 0.9, 0.0, 1.0, 1), 2 * 40 * 60
+    need = lib.lstmss_muon_workspace_bytes(ref(d))
+    names = ["W", "M", "dW", "Wo", "Mo", "ws"]
+    es = (4, 2)[dtype]
+    sizes = dict(W=n * es, M=n * 4, dW=n * 4, Wo=n * es, Mo=n * 4, ws=need)
+    call = lambda W, M, dW, Wo, Mo, ws: lib.lstmss_muon_update(  # noqa: E731
+        ref(d), ref(p), W, M, dW, Wo, Mo, ws, need, None)
+    refuses(call, names, sizes, ["Wo", "Mo"])
+    d.dtype = 0
+    names, sizes = ["G", "X", "ws"], dict(G=n * 4, X=n * 4, ws=need)
+    orth = lambda G, X, ws: lib.lstmss_orthogonalize(ref(d), G, X, ws, need, None)  # noqa: E731
+    refuses(orth, names, sizes, ["X"])
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_beams_refuse_memory_that_overlaps(lib, dtype):
+    S, K, V = 3, 4, 50
+    d, N, es = L.Beams(S, K, V, dtype), S * K, (4, 2)[dtype]
+    need = lib.lstmss_beam_workspace_bytes(ref(d))
+    names = ["logits", "scores", "done", "scores_out", "tokens", "parents", "done_out", "ws"]
+    sizes = dict.fromkeys(names, 4 * N)
+    sizes.update(logits=V * N * es, ws=need)
+    call = lambda logits, scores, done, scores_out, tokens, parents, done_out, ws: lib.lstmss_beam_step(  # noqa: E731
+        ref(d), logits, scores, 1, done, scores_out, tokens, parents, done_out, ws, need, None)
+    refuses(call, names, sizes, ["scores_out", "tokens", "parents", "done_out"])
+    names = ["parents", "x", "out"]
+    sizes = dict(parents=4 * N, x=7 * N * es, out=7 * N * es)
+    reorder = lambda parents, x, out: lib.lstmss_beam_reorder(7, N, K, dtype, parents, x, out, None)  # noqa: E731
+    refuses(reorder, names, sizes, ["out"])
+    names = ["tokens", "parents", "out"]
+    trace = lambda tokens, parents, out: lib.lstmss_beam_trace(7, N, K, tokens, parents, out, None)  # noqa: E731
+    refuses(trace, names, dict.fromkeys(names, 7 * N * 4), ["out"])
