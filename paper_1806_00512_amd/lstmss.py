@@ -702,6 +702,14 @@ def _sizes(T, B, I, V, dtype) -> Tokens:
     return Tokens(T, B, I, V, _dt(dtype))
 
 
+def _i32(v, name):
+    """v, a whole number of 32 bits (of a larger one the library would be given the low bits)."""
+    n = int(v)
+    if n != v or n >> 31 not in (0, -1):
+        raise ValueError("%s %r is not a whole number of 32 bits" % (name, v))
+    return n
+
+
 def _bytes(n, what):
     _check(0 if n >= 0 else int(n), what)
     return int(n)
@@ -948,13 +956,13 @@ NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
 def _orth(t, name, blocks, dtype, steps, abc) -> Orth:
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
         raise ValueError("%s must be [blocks * rows][cols]" % name)
-    blocks = int(blocks)
+    blocks = _i32(blocks, "blocks")
     if blocks < 1 or t.shape[0] % blocks:
         raise ValueError("%d rows are not %d blocks" % (t.shape[0], blocks))
     R, C = t.shape[0] // blocks, t.shape[1]
     if (R | C) >> 31:
         raise ValueError("sizes %s must be whole numbers of 31 bits" % ((R, C),))
-    return Orth(R, C, blocks, _dt(dtype), int(steps), *map(float, abc))
+    return Orth(R, C, blocks, _dt(dtype), _i32(steps, "steps"), *map(float, abc))
 
 
 def _orth_ws(d):
@@ -964,10 +972,10 @@ def _orth_ws(d):
 
 def muon_workspace_bytes(rows, cols, blocks=1) -> int:
     """Workspace of muon_update and orthogonalize on a matrix of `rows` rows in all."""
-    rows, blocks = int(rows), int(blocks)
+    rows, cols, blocks = (_i32(v, n) for v, n in ((rows, "rows"), (cols, "cols"), (blocks, "blocks")))
     if blocks < 1 or rows % blocks:
         raise ValueError("%d rows are not %d blocks" % (rows, blocks))
-    return _orth_ws(Orth(rows // blocks, int(cols), blocks, F32, 1, *NEWTON_SCHULZ))
+    return _orth_ws(Orth(rows // blocks, cols, blocks, F32, 1, *NEWTON_SCHULZ))
 
 
 def orthogonalize(G, blocks=1, steps=5, coefficients=NEWTON_SCHULZ, out=None, ws=None,
@@ -1019,14 +1027,14 @@ def _beams(S, K, V, dtype) -> Beams:
 
 def _sequences(N, K):
     """How many sequences of K beams N columns are."""
-    K = int(K)
+    K = _i32(K, "K")
     if K < 1 or N % K:
         raise ValueError("%d columns are not sequences of %d beams" % (N, K))
     return N // K, K
 
 
 def beam_workspace_bytes(S, K, V, dtype=F32) -> int:
-    d = _beams(int(S), int(K), int(V), dtype)
+    d = _beams(_i32(S, "S"), _i32(K, "K"), _i32(V, "V"), dtype)
     return _bytes(load().lstmss_beam_workspace_bytes(ctypes.byref(d)),
                   "lstmss_beam_workspace_bytes")
 
@@ -1043,7 +1051,7 @@ def beam_step(logits, scores, K, eos=-1, done=None, out=None, ws=None, stream=No
         raise ValueError("logits must be [V][N]")
     V, N = logits.shape
     S, K = _sequences(N, K)
-    dt, f32, i32, eos = logits.dtype, torch.float32, torch.int32, int(eos)
+    dt, f32, i32, eos = logits.dtype, torch.float32, torch.int32, _i32(eos, "eos")
     d = _beams(S, K, V, dt)
     o = dict(out) if out else {}
     for name in ("scores", "tokens", "parents") + (("done",) if eos >= 0 else ()):

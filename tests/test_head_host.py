@@ -252,3 +252,18 @@ def test_beams_refuse_memory_that_overlaps(lib, dtype):
     names = ["tokens", "parents", "out"]
     trace = lambda tokens, parents, out: lib.lstmss_beam_trace(7, N, K, tokens, parents, out, None)  # noqa: E731
     refuses(trace, names, dict.fromkeys(names, 7 * N * 4), ["out"])
+
+
+BIG = 1 << 32  # the low bits of BIG + 5 are 5
+
+
+@pytest.mark.parametrize("call", [
+    lambda: L.orthogonalize(z(6, 4), steps=BIG + 5), lambda: L.orthogonalize(z(6, 4), steps=4.5),
+    lambda: L.orthogonalize(z(6, 4), blocks=1.5), lambda: L.muon_update(z(6, 4), z(6, 4), z(6, 4), 0.1, steps=-BIG + 5),
+    lambda: L.muon_workspace_bytes(BIG + 6, 4), lambda: L.muon_workspace_bytes(6, BIG + 4),
+    lambda: L.beam_workspace_bytes(BIG + 1, 3, 7), lambda: L.beam_workspace_bytes(1, 3.5, 7),
+    lambda: L.beam_step(z(7, 6), z(6), 3, eos=BIG + 1), lambda: L.beam_step(z(7, 6), z(6), 3, eos=1.5),
+    lambda: L.beam_step(z(7, 6), z(6), 3.5), lambda: L.beam_reorder(z(5, 6), z(6, dtype=I32), 2.5)])
+def test_numbers_that_32_bits_do_not_hold(made, call):  # noqa: F811
+    with pytest.raises(ValueError):
+        call()
