@@ -321,10 +321,10 @@ struct Plan {
 // What a tile takes for a block of 16 k, in us, alone on its CU and where CUs have
 // several, and how much of its epilogue's time at a CU's share of memory is seen:
 // fitted to every tile and cut, measured on 31 products of 517 to 32000 rows, 640 to
-// 25600 columns and 494 to 4096 k, with and without z and residual.  Of these 62 the
-// estimates choose one within 1 % of the best for 48 and within 8 % for 60; for the two
-// of 517 x 1221 x 1023 one that is slower with operands in the caches (33 us for 30)
-// and quicker without (30.2 for 31.5).
+// 25600 columns and 494 to 4096 k, with and without z and residual.  Against all cuts
+// into 2 to 16, timed with operands in memory, the choice is within 1 % of the quickest
+// for 26 of the 32 fp32 calls and within 8 % for all (0.8 % in the mean), for 21 of the
+// 30 in bf16 within 1 %, for 27 within 8 % and for all within 11 %.
 struct TileCost {
     int rows, columns;
     float alone, shared; // us
@@ -334,7 +334,7 @@ constexpr TileCost COST_1[TILES] = {{256, 256, 0.33f, 0.45f, 1.25f},
                                     {256, 128, 0.25f, 0.23f, 1.f},
                                     {128, 128, 0.155f, 0.125f, 1.f},
                                     {64, 64, 0.055f, 0.052f, 0.75f}};
-constexpr TileCost COST_6[TILES] = {{}, {}, {128, 128, 0.64f, 0.47f, 1.f}, {64, 64, 0.23f, 0.165f, 0.75f}};
+constexpr TileCost COST_6[TILES] = {{}, {}, {128, 128, 0.64f, 0.47f, 1.f}, {64, 64, 0.26f, 0.165f, 0.75f}};
 
 // The least of estimated times of an M x N product over KS blocks of k in
 // `products` matrix instructions, whose epilogue moves `out` bytes an element (a
