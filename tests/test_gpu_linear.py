@@ -426,3 +426,28 @@ def test_refusals(L):
         L.linear_grad(x, W, dY, want=("dZ",))
     with pytest.raises(L.LstmssError):
         L.linear_grad(x, W, dY, ws=torch.empty(16, dtype=torch.uint8, device=DEV))
+
+
+def test_relu_gradients_against_differences_away_from_its_corner(L):
+    """Every second pre-activation above its corner and the others below it, by more than the
+    differences reach, where relu is linear.  All values are multiples of 2^-3 up to 2, h is 2^-7:
+    sums below 2^7 of multiples of 2^-10 are exact in fp32, and the differences are the gradients."""
+    T, B, K, N = 2, 5, 9, 6
+    x, W, r = make(T, B, K, N, "f32", 12)
+    x, W, b, c = (t.mul(8).round().div(8).clamp(-2, 2) for t in (x, W * 4, r(N), r(T, N, B)))
+    b += torch.where(torch.arange(N, device=DEV) % 2 == 0, 40.0, -40.0)
+    z, h = torch.empty(T, N, B, device=DEV), 2.0**-7
+    L.linear(x, W, b, act="relu", z=z)
+    assert 1 < float(z.abs().min()) and float(z.abs().max()) < 127 and bool((W != 0).any(1).all())
+    out = L.linear_grad(x, W, c, act="relu", z=z)
+
+    def loss(**change):
+        a = {"x": x, "W": W, "b": b, **change}
+        return float((c.double() * L.linear(a["x"], a["W"], a["b"], act="relu").double()).sum())
+
+    for name, t, g in (("x", x, out["dX"]), ("W", W, out["dW"]), ("b", b, out["db"])):
+        for i in range(t.numel()):
+            e = torch.zeros_like(t)
+            e.view(-1)[i] = h
+            assert (loss(**{name: t + e}) - loss(**{name: t - e})) / (2 * h) == float(g.view(-1)[i]), (name, i)
+    assert bool((out["db"][1::2] == 0).all()) and bool((out["dW"][::2] != 0).any(1).all())
