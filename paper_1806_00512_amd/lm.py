@@ -18,7 +18,8 @@ trained so go on bit for bit.  Weights are updated by SGD or, those of the layer
 and of the block with optimizer "muon", by orthogonalised momentum; generate()
 answers prompts by beam search.
 
-The rest are liblstmss calls on buffers allocated once.  `python -m
+The rest are liblstmss calls, a training step's on buffers allocated once (generate()
+allocates what an answer takes, step by step).  `python -m
 paper_1806_00512_amd.lm` trains a small model on synthetic sequences and lets it
 answer.
 """
